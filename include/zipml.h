@@ -348,6 +348,82 @@ int zipml_poly_rows(zipml_ctx* ctx, const zipml_dataset* grid, const uint8_t* co
                     const double* coef, const float* x, const float* scale, double* rows_out);
 int zipml_weighted_plane_mean(zipml_ctx* ctx, const zipml_dataset* grid, const uint8_t* plane, const double* c, float* g_out);
 
+/* Activations and a projection with low-rank adapters.  The paper quantizes the samples that a linear model is trained on; these
+ * calls do the same to what lies between the layers of a deeper one.  Dense matrices are row-major with a leading dimension in
+ * elements, of one of these types, aligned to their element (16-byte aligned rows are faster): */
+enum { ZIPML_F32 = 0, ZIPML_BF16 = 1, ZIPML_F16 = 2 };
+
+/* A matrix of activations in 8 bits.  Each row is cut into groups of `group` neighbouring features (the last one of a row may be
+ * shorter), each with a grid of its own: value = lo + code * step. */
+typedef struct zipml_checkpoint {
+    uint32_t struct_size;   /* sizeof(zipml_checkpoint)                                              */
+    int32_t group;          /* 32, 64, 128 or 256                                                    */
+    int64_t m, n;           /* rows, features                                                        */
+    int64_t row_bytes;      /* stride of codes, a multiple of 16, >= zipml_row_bytes(n, 8)           */
+    const uint8_t* codes;   /* m * row_bytes bytes, 16-byte aligned                                  */
+    const float* grids;     /* m * ceil(n / group) pairs (lo, step), 16-byte aligned                 */
+} zipml_checkpoint;
+
+/* zipml_checkpoint_encode: rounds X (m x n of type dtype, leading dimension ldx >= n) stochastically onto 8 bits, once, into the
+ *   caller's buffers behind the const pointers of `out` (codes fully written, padding zero).  A group's grid has 255 intervals
+ *   on its own range; a value goes to the lower or upper neighbouring level with the probabilities that make the
+ *   expectation equal to the value up to 2^-16 of an interval (paper Section 2.1), so a gradient that is linear in the
+ *   activations stays unbiased (the argument of Section 2.2).  Bits of Philox4x32-10 keyed by (seed, row, feature): the same
+ *   seed gives the same codes; take another for each matrix and step.  A NaN, an infinity or a group whose range overflows
+ *   fp32 makes the next zipml_sync() return ZIPML_ERR_NONFINITE (outputs undefined).
+ * zipml_checkpoint_decode: the values lo + code * step as `dtype`, rounded once.
+ * m = 0 is allowed and does nothing. */
+int zipml_checkpoint_encode(zipml_ctx* ctx, const void* X, int32_t dtype, int64_t m, int64_t n, int64_t ldx, uint64_t seed,
+                            const zipml_checkpoint* out);
+int zipml_checkpoint_decode(zipml_ctx* ctx, const zipml_checkpoint* data, int32_t dtype, void* X, int64_t ldx);
+
+/* Low-rank adapters and the requests that use them.  Adapter i adds b_i^T (scale_i a_i x) to what the projection makes of x.
+ * Request q holds the tokens starts[q] .. starts[q + 1] - 1 (starts ascending; a request may be empty) and uses adapter
+ * which[q], none where that is negative; several requests may use one adapter.  Tokens before starts[0] and from
+ * starts[requests] on belong to no request: every output row of theirs is left as it was. */
+typedef struct zipml_adapters {
+    uint32_t struct_size;   /* sizeof(zipml_adapters)                                                */
+    int32_t dtype;          /* ZIPML_BF16 or ZIPML_F16, of a and b and of the tokens                 */
+    int32_t count, rank;    /* adapters (1 .. 65535), their rank (1 .. 128)                          */
+    const void* a;          /* count x rank x inputs, contiguous                                     */
+    const void* b;          /* count x rank x outputs, contiguous                                    */
+    const float* scale;     /* count, or NULL: 1                                                     */
+    int32_t requests;       /* >= 1                                                                  */
+    int32_t reserved;       /* 0                                                                     */
+    const int32_t* starts;  /* requests + 1                                                          */
+    const int32_t* which;   /* requests; an index >= count counts as none and makes the next zipml_sync() return
+                               ZIPML_ERR_INVALID_ARG                                                 */
+} zipml_adapters;
+
+/* zipml_project: Y[t] = W^T x_t + b_i^T h_t with h_t = scale_i a_i x_t for the adapter i of token t.
+ *   weights   plane 1 of a dataset on a uniform grid, ZIPML_LAYOUT_ROWS: row k holds input k's weights, W[k][o] = feat_lo[o] +
+ *             code * feat_step[o], so a projection's weights are quantized by zipml_quantize on its inputs x outputs matrix
+ *             (plane 2 is not read).
+ *   adapters  NULL: the projection alone, and every token counts as in use.
+ *   X, Y      tokens x inputs and tokens x outputs of type dtype (ZIPML_BF16 or ZIPML_F16; adapters->dtype equal to it); not
+ *             overlapping.
+ *   hidden    NULL or tokens x rank floats: h_t, zero for requests without an adapter; what the backward pass needs.
+ * zipml_project_backward: for dY = the loss's gradient with respect to Y, with v_t = scale_i b_i dy_t,
+ *   dX[t] = W dy_t + a_i^T v_t             (tokens x inputs, dtype; NULL: not wanted)
+ *   grad_a[i] = sum of v_t (x) Q(x_t)      (count x rank x inputs floats; NULL: not wanted) over the tokens of adapter i, Q(x_t) from
+ *   grad_b[i] = sum of h_t (x) dy_t        `checkpoint` (its m >= tokens and n = inputs; may be NULL without grad_a); count x rank x
+ *                                          outputs floats; NULL: not wanted (hidden may then be NULL)
+ *   The gradients are written whole, zero for adapters without tokens.
+ * Products of 16-bit values and of codes are exact and summed in fp32; h_t and v_t are kept in fp32 and enter the second product as two
+ * 16-bit parts; dY times the outputs' steps is rounded to 11 bits once.  Results do not change from call to call.
+ * An infinity or a NaN in a token's row stays in that row (and in the gradients of its adapter); one in an adapter's factor b (backward: a)
+ * counts as zero in the product behind it and makes the next zipml_sync() return ZIPML_ERR_NONFINITE.
+ * tokens = 0 is allowed (gradients are then zero).  Workspace grows on a call that needs more than any before it; while the stream is being
+ * captured that is refused with ZIPML_ERR_WORKSPACE (make one call of that size first).  Earlier blocks live as long as the context, so
+ * recorded launches keep theirs; graphs recorded from one context share them and must not run at the same time.
+ * ZIPML_ERR_UNSUPPORTED: level tables, other layouts or types; ZIPML_ERR_WORKSPACE: inputs or outputs above 2^24, tokens above
+ * 2^30. */
+int zipml_project(zipml_ctx* ctx, const zipml_dataset* weights, const zipml_adapters* adapters, const void* X, int32_t dtype, int64_t tokens,
+                  int64_t ldx, void* Y, int64_t ldy, float* hidden);
+int zipml_project_backward(zipml_ctx* ctx, const zipml_dataset* weights, const zipml_adapters* adapters, const void* dY, int32_t dtype,
+                           int64_t tokens, int64_t lddy, const float* hidden, const zipml_checkpoint* checkpoint, void* dX, int64_t lddx,
+                           float* grad_a, float* grad_b);
+
 /* The end of a step on its own: x <- R(x - lr * Q4(g)) for a gradient g (n floats, device memory) that the caller has
  * formed, e.g. the sum of several devices' shares of a minibatch (paper "End-to-end Quantization" for Q4, the
  * l2-scaled sign-magnitude quantizer of the Supplement; Eq. (proxupdate) and the LS-SVM term for R).  Read from

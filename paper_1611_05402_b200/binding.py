@@ -19,11 +19,14 @@ NORM_L2, NORM_LINF = 0, 1
 REG_NONE, REG_L2, REG_L1, REG_NONNEG, REG_LSSVM = 0, 1, 2, 3, 4
 ENGINE_AUTO, ENGINE_STEPWISE, ENGINE_PERSISTENT, ENGINE_RING, ENGINE_LEAN, ENGINE_CLUSTER, ENGINE_STREAM, ENGINE_COLUMN, ENGINE_SOLO = 0, 1, 2, 3, 4, 5, 6, 7, 8
 
+F32, BF16, F16 = 0, 1, 2
+DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "csrc", "libzipml.so")
 EXPORTS = ["zipml_up_row_bytes", "zipml_shared_base_encode", "zipml_shared_base_decode", "zipml_loss_shared_base",
            "zipml_sgd_epoch_shared_base", "zipml_sgd_apply_gradient", "zipml_quantize_draw", "zipml_poly_rows", "zipml_weighted_plane_mean", "zipml_column_blocks_bytes", "zipml_convert_layout", "zipml_create", "zipml_destroy", "zipml_sync", "zipml_kernel_launches", "zipml_last_engine", "zipml_last_kernel", "zipml_barrier_latency", "zipml_wait_probe", "zipml_strerror", "zipml_row_bytes", "zipml_quantize",
            "zipml_optimal_levels", "zipml_sgd_epoch", "zipml_loss", "zipml_train_host",
-           "zipml_loss_codes_static"]
+           "zipml_loss_codes_static", "zipml_checkpoint_encode", "zipml_checkpoint_decode", "zipml_project", "zipml_project_backward"]
 
 
 class ZipmlError(RuntimeError):
@@ -57,6 +60,16 @@ class CSgdParams(C.Structure):
                 ("trace", C.c_void_p), ("reg", C.c_int32), ("reg_param", C.c_float),
                 ("model_out", C.c_void_p), ("cluster_contraction", C.c_int32), ("stream_prefetch", C.c_int32),
                 ("column_chunk_rows", C.c_int32), ("vector_norm", C.c_int32)]
+
+
+class CCheckpoint(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("group", C.c_int32), ("m", C.c_int64), ("n", C.c_int64), ("row_bytes", C.c_int64),
+                ("codes", C.c_void_p), ("grids", C.c_void_p)]
+
+
+class CAdapters(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("count", C.c_int32), ("rank", C.c_int32), ("a", C.c_void_p), ("b", C.c_void_p),
+                ("scale", C.c_void_p), ("requests", C.c_int32), ("reserved", C.c_int32), ("starts", C.c_void_p), ("which", C.c_void_p)]
 
 
 _lib = None
@@ -105,6 +118,11 @@ def lib():
         L.zipml_loss.argtypes = [vp, i32, vp, i64, i64, i64, C.POINTER(CDataset), vp, vp, vp]
         L.zipml_train_host.argtypes = [vp, vp, i64, i64, i64, vp, vp, i32, i32, i32, u64, C.POINTER(CSgdParams), i32, i32,
                                        vp]
+        L.zipml_checkpoint_encode.argtypes = [vp, vp, i32, i64, i64, i64, u64, C.POINTER(CCheckpoint)]
+        L.zipml_checkpoint_decode.argtypes = [vp, C.POINTER(CCheckpoint), i32, vp, i64]
+        L.zipml_project.argtypes = [vp, C.POINTER(CDataset), C.POINTER(CAdapters), vp, i32, i64, i64, vp, i64, vp]
+        L.zipml_project_backward.argtypes = [vp, C.POINTER(CDataset), C.POINTER(CAdapters), vp, i32, i64, i64, vp, C.POINTER(CCheckpoint), vp, i64,
+                                             vp, vp]
         L.zipml_loss_codes_static.argtypes = [C.c_int, vp, C.POINTER(CDataset), vp, vp, vp]
         _lib = L
     return _lib
@@ -124,6 +142,56 @@ def _ptr(t, dtype=None, device=None):
     if device is not None:
         assert t.device == device, f"expected a tensor on {device}, got {t.device}"
     return C.c_void_p(t.data_ptr())
+
+
+def _rows(t, device, dtypes=DTYPES):
+    """(pointer, dtype, rows, columns, leading dimension) of a matrix whose rows are contiguous."""
+    assert t.dim() == 2 and t.dtype in dtypes, f"expected a matrix of one of {sorted(map(str, dtypes))}, got {tuple(t.shape)} of {t.dtype}"
+    assert t.device == device, f"expected a tensor on {device}, got {t.device}"
+    assert t.shape[1] <= 1 or t.stride(1) == 1, "rows must be contiguous"
+    ld = t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    return C.c_void_p(t.data_ptr()), DTYPES[t.dtype], t.shape[0], t.shape[1], ld
+
+
+class Checkpoint:
+    """Activations in 8 bits (see zipml_checkpoint): codes (m, row_bytes) uint8, grids (m, groups, 2) float32."""
+
+    def __init__(self, codes, grids, m, n, group):
+        assert codes.dtype == torch.uint8 and grids.dtype == torch.float32 and codes.is_contiguous() and grids.is_contiguous()
+        assert codes.dim() == 2 and codes.shape[0] >= m and grids.numel() >= m * -(-n // group) * 2 and codes.device == grids.device
+        self.codes, self.grids, self.m, self.n, self.group, self.row_bytes = codes, grids, m, n, group, codes.shape[1]
+
+    def c_struct(self):
+        d = CCheckpoint()
+        d.struct_size = C.sizeof(CCheckpoint)
+        d.group, d.m, d.n, d.row_bytes = self.group, self.m, self.n, self.row_bytes
+        d.codes, d.grids = self.codes.data_ptr(), self.grids.data_ptr()
+        return d
+
+    @property
+    def packed_bytes(self):
+        return self.m * self.row_bytes + 8 * self.m * -(-self.n // self.group)
+
+
+class Adapters:
+    """Low-rank adapters (see zipml_adapters): a (count, rank, inputs), b (count, rank, outputs), scale (count,) float32 or None."""
+
+    def __init__(self, a, b, scale=None):
+        assert a.dim() == b.dim() == 3 and a.shape[:2] == b.shape[:2] and a.dtype == b.dtype and a.device == b.device
+        assert a.is_contiguous() and b.is_contiguous()
+        assert scale is None or (scale.dtype == torch.float32 and scale.is_contiguous() and scale.numel() == a.shape[0] and scale.device == a.device)
+        self.a, self.b, self.scale = a, b, scale
+
+    def c_struct(self, starts, which):
+        """With the requests that use them: starts (requests + 1,) and which (requests,), int32 on the device."""
+        assert starts.dtype == which.dtype == torch.int32 and starts.is_contiguous() and which.is_contiguous()
+        assert starts.device == which.device == self.a.device and starts.numel() == which.numel() + 1
+        d = CAdapters()
+        d.struct_size = C.sizeof(CAdapters)
+        d.dtype, d.count, d.rank, d.requests = DTYPES.get(self.a.dtype, -1), self.a.shape[0], self.a.shape[1], which.numel()
+        d.a, d.b, d.starts, d.which = self.a.data_ptr(), self.b.data_ptr(), starts.data_ptr(), which.data_ptr()
+        d.scale = self.scale.data_ptr() if self.scale is not None else None
+        return d
 
 
 class Dataset:
@@ -430,6 +498,78 @@ class Context:
                                   _ptr(x, torch.float32, self.device), _ptr(out))
         _check(rc, "zipml_loss")
         return out
+
+    def zipml_checkpoint_encode(self, X, group=128, seed=0, out=None):
+        """X (m, n) fp32, bf16 or fp16 -> Checkpoint (or into `out`, one of the same shape and group)."""
+        ptr, dtype, m, n, ld = _rows(X, self.device)
+        if out is None:
+            out = Checkpoint(torch.empty((m, (n + 15) // 16 * 16), dtype=torch.uint8, device=self.device),
+                             torch.empty((m, -(-n // group), 2), dtype=torch.float32, device=self.device), m, n, group)
+        assert out.codes.device == self.device
+        d = out.c_struct()
+        _check(lib().zipml_checkpoint_encode(self._h, ptr, dtype, m, n, ld, seed, C.byref(d)), "zipml_checkpoint_encode")
+        return out
+
+    def zipml_checkpoint_decode(self, data, dtype=torch.bfloat16, out=None):
+        """The checkpoint's values as (m, n) of `dtype` (or into `out`, of its own type)."""
+        out = torch.empty((data.m, data.n), dtype=dtype, device=self.device) if out is None else out
+        ptr, kind, m, n, ld = _rows(out, self.device)
+        assert (m, n) == (data.m, data.n) and data.codes.device == self.device
+        d = data.c_struct()
+        _check(lib().zipml_checkpoint_decode(self._h, C.byref(d), kind, ptr, ld), "zipml_checkpoint_decode")
+        return out
+
+    def _adapters(self, weights, adapters, starts, which):
+        assert weights.plane1.device == self.device
+        if adapters is None:
+            return None
+        assert adapters.a.device == self.device and adapters.a.shape[2] == weights.m and adapters.b.shape[2] == weights.n
+        return adapters.c_struct(starts, which)
+
+    def zipml_project(self, weights, X, adapters=None, starts=None, which=None, out=None, hidden=None):
+        """X (tokens, inputs) bf16 or fp16 through the projection `weights` (a Dataset of inputs x outputs) and each request's adapter ->
+        (tokens, outputs).  hidden: optional (tokens, rank) fp32, what the backward pass needs of the adapters.  Rows of tokens
+        outside the requests are left as they were (uninitialised in a new result)."""
+        ptr, dtype, tokens, n_in, ld = _rows(X, self.device)
+        assert n_in == weights.m
+        out = torch.empty((tokens, weights.n), dtype=X.dtype, device=self.device) if out is None else out
+        optr, odtype, orows, ocols, old = _rows(out, self.device)
+        assert (orows, ocols, odtype) == (tokens, weights.n, dtype)
+        a = self._adapters(weights, adapters, starts, which)
+        assert hidden is None or (adapters is not None and hidden.shape == (tokens, adapters.a.shape[1]))
+        w = weights.c_struct()
+        _check(lib().zipml_project(self._h, C.byref(w), None if a is None else C.byref(a), ptr, dtype, tokens, ld, optr, old,
+                                   _ptr(hidden, torch.float32, self.device)), "zipml_project")
+        return out
+
+    def zipml_project_backward(self, weights, dY, adapters=None, starts=None, which=None, hidden=None, checkpoint=None, out=None, grad_a=None,
+                               grad_b=None, want_input=True):
+        """Gradients of zipml_project from dY (tokens, outputs): (dX, grad_a, grad_b), the last two fp32 and None without adapters; grad_a
+        also without `checkpoint`, grad_b without `hidden`, dX without want_input."""
+        ptr, dtype, tokens, n_out, ld = _rows(dY, self.device)
+        assert n_out == weights.n
+        optr, old = None, 0
+        if want_input:
+            out = torch.empty((tokens, weights.m), dtype=dY.dtype, device=self.device) if out is None else out
+            optr, odtype, orows, ocols, old = _rows(out, self.device)
+            assert (orows, ocols, odtype) == (tokens, weights.m, dtype)
+        else:
+            out = None
+        a = self._adapters(weights, adapters, starts, which)
+        if adapters is not None and checkpoint is not None and grad_a is None:
+            grad_a = torch.empty(adapters.a.shape, dtype=torch.float32, device=self.device)
+        if adapters is not None and hidden is not None and grad_b is None:
+            grad_b = torch.empty(adapters.b.shape, dtype=torch.float32, device=self.device)
+        assert hidden is None or (adapters is not None and hidden.shape == (tokens, adapters.a.shape[1]))
+        assert grad_a is None or (adapters is not None and grad_a.shape == adapters.a.shape)
+        assert grad_b is None or (adapters is not None and grad_b.shape == adapters.b.shape)
+        assert checkpoint is None or checkpoint.codes.device == self.device
+        w, c = weights.c_struct(), None if checkpoint is None else checkpoint.c_struct()
+        f32 = torch.float32
+        _check(lib().zipml_project_backward(self._h, C.byref(w), None if a is None else C.byref(a), ptr, dtype, tokens, ld, _ptr(hidden, f32, self.device),
+                                            None if c is None else C.byref(c), optr, old, _ptr(grad_a, f32, self.device),
+                                            _ptr(grad_b, f32, self.device)), "zipml_project_backward")
+        return out, grad_a, grad_b
 
     def zipml_train_host(self, A_host, b_host, x_host, bits, batch, lr, epochs, optimal_levels=False, hist_bins=1024,
                          quantize_seed=0, lr_decay=False, **kw):

@@ -3,6 +3,7 @@
 
 #include "common.cuh"
 #include "internal.h"
+#include "project.cuh"
 
 namespace zipml {
 
@@ -27,6 +28,31 @@ static int grow(unsigned char** buf, size_t* have, size_t want, cudaStream_t str
 
 int ws_reserve(zipml_ctx* ctx, size_t bytes) { return grow(&ctx->ws, &ctx->ws_bytes, bytes, ctx->stream); }
 int stage_reserve(zipml_ctx* ctx, size_t bytes) { return grow(&ctx->stage, &ctx->stage_bytes, bytes, ctx->stream); }
+
+bool capturing(zipml_ctx* ctx) {
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(ctx->stream, &capture) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return true;
+    }
+    return capture != cudaStreamCaptureStatusNone;
+}
+
+int project_reserve(zipml_ctx* ctx, size_t bytes, unsigned char** block) {
+    if (bytes > ctx->project_bytes || ctx->project_blocks == 0) {
+        if (capturing(ctx) || ctx->project_blocks == zipml_ctx::kProjectBlocks) return ZIPML_ERR_WORKSPACE;
+        size_t want = bytes > 2 * ctx->project_bytes ? bytes : 2 * ctx->project_bytes;
+        want = (want + (1u << 20) - 1) >> 20 << 20;
+        if (want == 0) want = 1u << 20;
+        unsigned char* fresh = nullptr;
+        const cudaError_t e = cudaMalloc(reinterpret_cast<void**>(&fresh), want);
+        if (e != cudaSuccess) return cuda_status(e);
+        ctx->project_ws[ctx->project_blocks++] = fresh;
+        ctx->project_bytes = want;
+    }
+    *block = ctx->project_ws[ctx->project_blocks - 1];
+    return ZIPML_OK;
+}
 
 bool early_start(zipml_ctx* ctx, int64_t steps, cudaLaunchAttribute* attr) {
     if (steps > kEarlySteps) return false;
@@ -88,6 +114,41 @@ int check_dataset(const zipml_dataset* d) {
 }
 
 constexpr int kLossPartials = 4096;
+
+constexpr int64_t kMostColumns = 1 << 24, kMostTokens = 1 << 30;
+
+static int element_size(int32_t dtype) { return dtype == ZIPML_F32 ? 4 : dtype == ZIPML_BF16 || dtype == ZIPML_F16 ? 2 : 0; }
+static bool aligned_to(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes == 0; }
+
+static int check_checkpoint(const zipml_checkpoint* c) {
+    if (!c || c->struct_size != sizeof(zipml_checkpoint)) return ZIPML_ERR_INVALID_ARG;
+    if (c->group != 32 && c->group != 64 && c->group != 128 && c->group != 256) return ZIPML_ERR_UNSUPPORTED;
+    if (c->m < 0 || c->n <= 0 || c->row_bytes % 16 != 0 || c->row_bytes < zipml_row_bytes(c->n, 8)) return ZIPML_ERR_INVALID_ARG;
+    if (c->row_bytes > 0x7fffffffLL - 256) return ZIPML_ERR_WORKSPACE;
+    if (c->m > 0 && (!c->codes || !c->grids || !aligned16(c->codes) || !aligned16(c->grids))) return ZIPML_ERR_INVALID_ARG;
+    return ZIPML_OK;
+}
+
+// What both directions of a projection ask of their arguments.
+static int check_projection(const zipml_dataset* w, const zipml_adapters* a, int32_t dtype, int64_t tokens) {
+    const int rc = check_dataset(w);
+    if (rc != ZIPML_OK) return rc;
+    if (w->level_mode != ZIPML_LEVELS_UNIFORM || w->layout != ZIPML_LAYOUT_ROWS) return ZIPML_ERR_UNSUPPORTED;
+    if (dtype != ZIPML_BF16 && dtype != ZIPML_F16) return dtype == ZIPML_F32 ? ZIPML_ERR_UNSUPPORTED : ZIPML_ERR_INVALID_ARG;
+    if (tokens < 0) return ZIPML_ERR_INVALID_ARG;
+    if (tokens > kMostTokens || w->m > kMostColumns || w->n > kMostColumns) return ZIPML_ERR_WORKSPACE;
+    if (!a) return ZIPML_OK;
+    if (a->struct_size != sizeof(zipml_adapters) || a->reserved != 0) return ZIPML_ERR_INVALID_ARG;
+    if (a->dtype != dtype) return ZIPML_ERR_INVALID_ARG;
+    if (a->count < 1 || a->rank < 1 || a->requests < 1) return ZIPML_ERR_INVALID_ARG;
+    if (a->count > 65535 || a->rank > kMaxRank || a->requests > (1 << 30)) return ZIPML_ERR_UNSUPPORTED;
+    if (!a->a || !a->b || !a->starts || !a->which || !aligned_to(a->a, 2) || !aligned_to(a->b, 2) || !aligned_to(a->starts, 4) || !aligned_to(a->which, 4) ||
+        !aligned_to(a->scale, 4))
+        return ZIPML_ERR_INVALID_ARG;
+    return ZIPML_OK;
+}
+
+static float code_center(int bits) { return (float)(1 << (container_bits(bits) - 1)); }
 
 }  // namespace zipml
 
@@ -191,6 +252,7 @@ int zipml_destroy(zipml_ctx* ctx) {
     if (ctx->stage) (void)cudaFree(ctx->stage);
     if (ctx->exchange) (void)cudaFree(ctx->exchange);
     if (ctx->range_keys) (void)cudaFree(ctx->range_keys);
+    for (int i = 0; i < ctx->project_blocks; ++i) (void)cudaFree(ctx->project_ws[i]);
     if (ctx->d_status) (void)cudaFree(ctx->d_status);
     (void)cudaGetLastError();
     delete ctx;
@@ -651,6 +713,148 @@ int zipml_train_host(zipml_ctx* ctx, const float* A_host, int64_t m, int64_t n, 
     if (e == cudaSuccess) e = cudaMemcpyAsync(loss_out_host, dloss, sizeof(double), cudaMemcpyDeviceToHost, ctx->stream);
     if (e != cudaSuccess) return cuda_status(e);
     return zipml_sync(ctx);
+}
+
+int zipml_checkpoint_encode(zipml_ctx* ctx, const void* X, int32_t dtype, int64_t m, int64_t n, int64_t ldx, uint64_t seed,
+                            const zipml_checkpoint* out) {
+    if (!ctx) return ZIPML_ERR_INVALID_ARG;
+    const int rc = check_checkpoint(out);
+    if (rc != ZIPML_OK) return rc;
+    const int size = element_size(dtype);
+    if (size == 0 || m != out->m || n != out->n || ldx < n) return ZIPML_ERR_INVALID_ARG;
+    if (m == 0) return ZIPML_OK;
+    if (!X || !aligned_to(X, size)) return ZIPML_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return ZIPML_ERR_CUDA;
+    return launch_checkpoint_encode(ctx, X, dtype, m, n, ldx, seed, out);
+}
+
+int zipml_checkpoint_decode(zipml_ctx* ctx, const zipml_checkpoint* data, int32_t dtype, void* X, int64_t ldx) {
+    if (!ctx) return ZIPML_ERR_INVALID_ARG;
+    const int rc = check_checkpoint(data);
+    if (rc != ZIPML_OK) return rc;
+    const int size = element_size(dtype);
+    if (size == 0 || ldx < data->n) return ZIPML_ERR_INVALID_ARG;
+    if (data->m == 0) return ZIPML_OK;
+    if (!X || !aligned_to(X, size)) return ZIPML_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return ZIPML_ERR_CUDA;
+    return launch_checkpoint_decode(ctx, data, dtype, X, ldx);
+}
+
+int zipml_project(zipml_ctx* ctx, const zipml_dataset* weights, const zipml_adapters* adapters, const void* X, int32_t dtype, int64_t tokens,
+                  int64_t ldx, void* Y, int64_t ldy, float* hidden) {
+    if (!ctx) return ZIPML_ERR_INVALID_ARG;
+    int rc = check_projection(weights, adapters, dtype, tokens);
+    if (rc != ZIPML_OK) return rc;
+    if (ldx < weights->m || ldy < weights->n || (hidden && !adapters) || !aligned_to(hidden, 4)) return ZIPML_ERR_INVALID_ARG;
+    if (tokens == 0) return ZIPML_OK;
+    if (!X || !Y || X == Y || !aligned_to(X, 2) || !aligned_to(Y, 2)) return ZIPML_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return ZIPML_ERR_CUDA;
+    // tensor copies want rows 16 bytes aligned: the first stage makes a copy of others on its way
+    const bool copy = !aligned16(X) || ldx % 8 != 0;
+    const int64_t ld_copy = (weights->m + 7) / 8 * 8;
+    const int rank = adapters ? adapters->rank : 0;
+    size_t bytes = 3 * carve_size(sizeof(float) * (size_t)tokens);
+    if (!hidden) bytes += carve_size(sizeof(float) * (size_t)tokens * rank);
+    if (copy) bytes += carve_size(2 * (size_t)tokens * (size_t)ld_copy);
+    unsigned char* ws = nullptr;
+    rc = project_reserve(ctx, bytes, &ws);
+    if (rc != ZIPML_OK) return rc;
+    Carver carve(ws);
+    ShrinkArgs s{};
+    s.z = X; s.tokens = tokens; s.ldz = ldx; s.columns = (int)weights->m;
+    s.ids = carve.take<int>((size_t)tokens);
+    s.sum = carve.take<float>((size_t)tokens);
+    s.hidden_scale = carve.take<float>((size_t)tokens);
+    if (adapters) {
+        s.down = adapters->a; s.scale = adapters->scale; s.starts = adapters->starts; s.which = adapters->which;
+        s.requests = adapters->requests; s.adapters = adapters->count; s.rank = rank;
+        s.hidden = hidden ? hidden : carve.take<float>((size_t)tokens * rank);
+    }
+    if (copy) { s.copy = carve.take<uint16_t>((size_t)tokens * (size_t)ld_copy); s.ld_copy = ld_copy; }
+    s.status = ctx->d_status;
+    rc = launch_shrink(ctx, s, dtype, false);
+    if (rc != ZIPML_OK) return rc;
+    ProjectArgs p{};
+    p.tokens = tokens; p.features = (int)weights->n; p.depth = (int)weights->m; p.bits = container_bits(weights->bits);
+    p.lo = weights->feat_lo; p.step = weights->feat_step; p.center = code_center(weights->bits);
+    p.ids = s.ids; p.sum = s.sum; p.hidden_scale = s.hidden_scale; p.hidden = s.hidden;
+    p.up = adapters ? adapters->b : nullptr; p.rank = rank;
+    p.out = Y; p.ldo = ldy; p.out_bf16 = dtype == ZIPML_BF16;
+    p.early = capturing(ctx) ? 0 : copy ? 3 : 1;
+    p.status = ctx->d_status;
+    return launch_project(ctx, p, copy ? s.copy : X, copy ? ld_copy : ldx, dtype == ZIPML_BF16, weights, false);
+}
+
+int zipml_project_backward(zipml_ctx* ctx, const zipml_dataset* weights, const zipml_adapters* adapters, const void* dY, int32_t dtype,
+                           int64_t tokens, int64_t lddy, const float* hidden, const zipml_checkpoint* checkpoint, void* dX, int64_t lddx,
+                           float* grad_a, float* grad_b) {
+    if (!ctx) return ZIPML_ERR_INVALID_ARG;
+    int rc = check_projection(weights, adapters, dtype, tokens);
+    if (rc != ZIPML_OK) return rc;
+    if (lddy < weights->n || (dX && lddx < weights->m) || ((grad_a || grad_b) && !adapters)) return ZIPML_ERR_INVALID_ARG;
+    if (!aligned_to(hidden, 4) || !aligned_to(grad_a, 4) || !aligned_to(grad_b, 4) || !aligned_to(dX, 2) || !aligned_to(dY, 2)) return ZIPML_ERR_INVALID_ARG;
+    if (grad_a || checkpoint) {
+        rc = check_checkpoint(checkpoint);
+        if (rc != ZIPML_OK) return rc;
+        if (checkpoint->n != weights->m || checkpoint->m < tokens) return ZIPML_ERR_INVALID_ARG;
+    }
+    if (tokens > 0 && (!dY || dY == dX || (grad_b && !hidden))) return ZIPML_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return ZIPML_ERR_CUDA;
+    const int rank = adapters ? adapters->rank : 0;
+    const int64_t ld_scaled = (weights->n + 7) / 8 * 8;
+    float* v = nullptr;
+    if (tokens > 0 && (dX || grad_a)) {
+        const size_t bytes = 4 * carve_size(sizeof(float) * (size_t)tokens) + carve_size(sizeof(float) * (size_t)tokens * rank) +
+                             (dX ? carve_size(2 * (size_t)tokens * (size_t)ld_scaled) : 0);
+        unsigned char* ws = nullptr;
+        rc = project_reserve(ctx, bytes, &ws);
+        if (rc != ZIPML_OK) return rc;
+        Carver carve(ws);
+        ShrinkArgs s{};
+        s.z = dY; s.tokens = tokens; s.ldz = lddy; s.columns = (int)weights->n;
+        s.ids = carve.take<int>((size_t)tokens);
+        s.sum = carve.take<float>((size_t)tokens);
+        s.hidden_scale = carve.take<float>((size_t)tokens);
+        s.row_scale = carve.take<float>((size_t)tokens);
+        if (adapters) {
+            s.down = adapters->b; s.scale = adapters->scale; s.starts = adapters->starts; s.which = adapters->which;
+            s.requests = adapters->requests; s.adapters = adapters->count; s.rank = rank;
+            s.hidden = v = carve.take<float>((size_t)tokens * rank);
+        }
+        s.lo = weights->feat_lo; s.step = weights->feat_step; s.center = code_center(weights->bits);
+        if (dX) { s.scaled = reinterpret_cast<__half*>(carve.take<uint16_t>((size_t)tokens * (size_t)ld_scaled)); s.ld_scaled = ld_scaled; }
+        s.status = ctx->d_status;
+        rc = launch_shrink(ctx, s, dtype, true);
+        if (rc != ZIPML_OK) return rc;
+        if (dX) {
+            ProjectArgs p{};
+            p.tokens = tokens; p.features = (int)weights->m; p.depth = (int)weights->n; p.bits = container_bits(weights->bits);
+            p.center = s.center;
+            p.ids = s.ids; p.sum = s.sum; p.row_scale = s.row_scale; p.hidden_scale = s.hidden_scale; p.hidden = v;
+            p.up = adapters ? adapters->a : nullptr; p.rank = rank;
+            p.out = dX; p.ldo = lddx; p.out_bf16 = dtype == ZIPML_BF16;
+            p.early = capturing(ctx) ? 0 : 3;
+            p.status = ctx->d_status;
+            rc = launch_project(ctx, p, s.scaled, ld_scaled, false, weights, true);
+            if (rc != ZIPML_OK) return rc;
+        }
+    }
+    if (!grad_a && !grad_b) return ZIPML_OK;
+    GradArgs g{};
+    g.tokens = tokens; g.starts = adapters->starts; g.which = adapters->which; g.requests = adapters->requests; g.adapters = adapters->count; g.rank = rank;
+    g.v = v; g.hidden = hidden;
+    if (checkpoint) {
+        g.codes = checkpoint->codes; g.code_stride = checkpoint->row_bytes; g.grids = reinterpret_cast<const float2*>(checkpoint->grids);
+        g.group = checkpoint->group; g.groups = (int)((checkpoint->n + checkpoint->group - 1) / checkpoint->group);
+    }
+    g.inputs = (int)weights->m; g.outputs = (int)weights->n; g.dy = dY; g.lddy = lddy; g.bf16 = dtype == ZIPML_BF16;
+    g.grad_down = grad_a; g.grad_up = grad_b;
+    g.status = ctx->d_status;
+    return launch_project_grad(ctx, g);
 }
 
 }  // extern "C"

@@ -34,6 +34,12 @@ struct zipml_ctx {
     const char* last_kernel = "";
     void ran(int engine, const char* kernel) { last_engine = engine; last_kernel = kernel; }
     void* tmap_encode = nullptr;    // cuTensorMapEncodeTiled, resolved on first use
+    // workspace of the projections: its blocks live as long as the context (recorded launches hold their addresses), the last one is
+    // the largest, each at least twice the one before
+    static constexpr int kProjectBlocks = 44;
+    unsigned char* project_ws[kProjectBlocks] = {};
+    int project_blocks = 0;
+    size_t project_bytes = 0;
 };
 
 namespace zipml {
@@ -45,6 +51,8 @@ int check_dataset(const zipml_dataset* d);
 int cuda_status(cudaError_t e);                       // ZIPML_OK or ZIPML_ERR_CUDA (clears the sticky error)
 int ws_reserve(zipml_ctx* ctx, size_t bytes);         // grow ctx->ws to at least `bytes`
 int stage_reserve(zipml_ctx* ctx, size_t bytes);
+int project_reserve(zipml_ctx* ctx, size_t bytes, unsigned char** block);   // ZIPML_ERR_WORKSPACE where it would have to grow during capture
+bool capturing(zipml_ctx* ctx);                       // the context's stream is being recorded into a graph
 // `bytes` of exchange words between clusters, and the tag of the first of `steps` steps.  At most two buffers in turn, 8 clusters, 16
 // bytes for each of 8,192 features and what the last slice or column has past them.
 constexpr size_t kExchangeBytes = 2 * 8 * (8192 + 1024) * 16;

@@ -1,0 +1,83 @@
+// Fifth-generation tensor core instructions (tcgen05), tensor copies and waits bounded in time, as thin wrappers.
+#pragma once
+
+#include "sgd_common.cuh"
+
+namespace zipml {
+
+constexpr unsigned long long kTcWaitNs = 2000000000ull;       // a wait that takes longer gives up
+
+__device__ __forceinline__ unsigned long long global_ns() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+
+// Waits for a phase of a shared-memory barrier; false, with ZIPML_ERR_TIMEOUT recorded, after kTcWaitNs, or once another thread
+// of the block has given up.
+__device__ __noinline__ bool tc_wait_long(uint64_t* bar, uint32_t parity, volatile int* gave_up, DeviceStatus* status, int where) {
+    const unsigned long long began = global_ns();
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i)
+            if (mbar_try_wait(bar, parity)) return true;
+        if (*gave_up) return false;
+        if (global_ns() - began > kTcWaitNs) break;
+    }
+    *gave_up = 1;
+    set_status(status, ZIPML_ERR_TIMEOUT, where);
+    return false;
+}
+__device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, volatile int* gave_up, DeviceStatus* status, int where) {
+    return mbar_try_wait(bar, parity) || tc_wait_long(bar, parity, gave_up, status, where);
+}
+// The same for a block that has given up and still has copies or products in flight.
+__device__ __noinline__ void tc_drain(uint64_t* bar, uint32_t parity) {
+    const unsigned long long began = global_ns();
+    while (!mbar_try_wait(bar, parity) && global_ns() - began < kTcWaitNs) {}
+}
+
+__device__ __forceinline__ void tc_copy_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+}
+
+// Shared-memory operand with the 128-byte swizzle.  Depth-major (K): rows of 128 bytes, 8 of them `sbo` apart.  Row-major (MN): 64
+// values of the outer dimension are 128 bytes, the next 64 `lbo` on, 8 of the depth `sbo` apart.
+__device__ __forceinline__ uint64_t tc_operand(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// 16-bit operands (both bf16 or both fp16), fp32 sums, 128 x n x 16; `a_outer`: A is stored row-major (MN).
+__host__ __device__ constexpr uint32_t tc_kind(bool bf16, bool a_outer, int n) {
+    return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (a_outer ? 1u << 15 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, bool accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"((uint32_t)accumulate) : "memory");
+}
+// Arrives on `bar` once every product issued so far by this thread has ended.
+__device__ __forceinline__ void tc_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tc_alloc(uint32_t* slot, uint32_t columns) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tc_free(uint32_t tmem, uint32_t columns) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// Makes this thread's ordinary shared-memory stores visible to the tensor cores and the copy engine.
+__device__ __forceinline__ void tc_publish() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// 16 columns of this warp's 32 lanes of tensor memory.
+__device__ __forceinline__ void tc_load16(uint32_t tmem, uint32_t (&v)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+                   "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(tmem));
+}
+__device__ __forceinline__ void tc_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+}  // namespace zipml

@@ -1,0 +1,669 @@
+"""Checkpoints of activations and projections with low-rank adapters, through the public calls, against plain 64-bit arithmetic.
+
+Tolerances count roundings.  eps/2 is the half step of the output's type.  A sum of k products in fp32 is off by at most k steps of
+2^-23 (tensor cores cut instead of rounding) of the sum of the products' magnitudes, which the references return beside the value.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1611_05402_b200 import binding
+
+gpu = pytest.mark.gpu
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    with binding.Context("cuda:0") as c:
+        yield c
+
+
+def half_step(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+# --- plain forms ----------------------------------------------------------------------------------------------------------------
+
+def philox(c0, c1, c2, c3, k0, k1):
+    """Philox4x32-10 on uint64 arrays that hold 32-bit words."""
+    m = np.uint64(0xFFFFFFFF)
+    c = [np.asarray(v, dtype=np.uint64) for v in (c0, c1, c2, c3)]
+    k0, k1 = int(k0), int(k1)
+    for _ in range(10):
+        p0, p1 = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(p1 >> np.uint64(32)) ^ c[1] ^ np.uint64(k0), p1 & m, (p0 >> np.uint64(32)) ^ c[3] ^ np.uint64(k1), p0 & m]
+        k0, k1 = (k0 + 0x9E3779B9) & 0xFFFFFFFF, (k1 + 0xBB67AE85) & 0xFFFFFFFF
+    return c
+
+
+def plain_encode(x, group, seed):
+    """(codes, lo, step) with every operation one fp32 rounding, and the draws of the stated generator."""
+    x = x.float().cpu().numpy()
+    m, n = x.shape
+    rows, blocks = np.arange(m, dtype=np.uint64)[:, None], np.arange(-(-n // 8), dtype=np.uint64)[None, :]
+    zero = np.zeros((m, blocks.shape[1]), dtype=np.uint64)
+    words = philox(blocks + zero, rows + zero, zero, zero + np.uint64(8), seed & 0xFFFFFFFF, seed >> 32)
+    draws = np.stack([h for w in words for h in (w & np.uint64(0xFFFF), w >> np.uint64(16))], 2).reshape(m, -1)[:, :n].astype(np.int64)
+    codes, grids = np.zeros((m, n), dtype=np.uint8), np.zeros((m, -(-n // group), 2), dtype=np.float32)
+    for g in range(grids.shape[1]):
+        part = x[:, g * group:(g + 1) * group]
+        lo, hi = part.min(1, keepdims=True), part.max(1, keepdims=True)
+        span = hi - lo
+        with np.errstate(divide="ignore", over="ignore"):
+            inv = np.where(span > 0, np.minimum(np.float32(255) / span, np.finfo(np.float32).max), np.float32(0))
+        t = np.clip((part - lo) * inv, np.float32(0), np.float32(255))
+        codes[:, g * group:(g + 1) * group] = (np.ceil(t * np.float32(65536)).astype(np.int64) + draws[:, g * group:(g + 1) * group]) >> 16
+        grids[:, g, 0], grids[:, g, 1] = lo[:, 0], (span / np.float32(255))[:, 0]
+    return codes, grids
+
+
+def checkpoint_values(cp):
+    lo, step = (cp.grids[:, :, i].double().repeat_interleave(cp.group, 1)[:, :cp.n] for i in (0, 1))
+    return lo, step, cp.codes[:, :cp.n].double()
+
+
+def weight_parts(ds):
+    """(beta, step, code - centre) in 64 bits: W = beta + step * (code - centre)."""
+    cb = {1: 2, 2: 2, 3: 4, 4: 4}.get(ds.bits, 8)
+    shifts = torch.arange(8 // cb, device=ds.plane1.device, dtype=torch.uint8) * cb
+    codes = ((ds.plane1[:, :, None] >> shifts) & ((1 << cb) - 1)).reshape(ds.m, -1)[:, :ds.n].double()
+    centre = float(1 << (cb - 1))
+    return ds.feat_lo.double() + centre * ds.feat_step.double(), ds.feat_step.double(), codes - centre
+
+
+def owners(starts, which, tokens, count):
+    """Adapter of each token: kNone (-1) or -2 outside the requests."""
+    ids = np.full(tokens, -2)
+    s = starts.tolist()
+    for q, i in enumerate(which.tolist()):
+        ids[max(s[q], 0):max(min(s[q + 1], tokens), 0)] = i if 0 <= i < count else -1
+    return ids
+
+
+class Problem:
+    """A projection with its adapters, and what the plain forms say about it."""
+
+    def __init__(self, ctx, tokens, inputs, outputs, bits, dtype, rank, count, lengths, which=None, group=128, seed=0, scale=True, ldx=None, first=0):
+        g = torch.Generator().manual_seed(seed)
+        dev = ctx.device
+        W = torch.randn(inputs, outputs, generator=g) / math.sqrt(inputs)
+        self.weights = ctx.zipml_quantize(W.to(dev), bits, seed=seed + 1)
+        self.tokens, self.dtype, self.group = tokens, dtype, group
+        ld = inputs if ldx is None else ldx
+        self.x = torch.randn(tokens, ld, generator=g).to(dtype).to(dev)[:, :inputs]
+        self.dy = torch.randn(tokens, outputs, generator=g).to(dtype).to(dev)
+        self.count, self.rank = count, rank
+        if count:
+            self.a = (torch.randn(count, rank, inputs, generator=g) / math.sqrt(inputs)).to(dtype).to(dev)
+            self.b = (torch.randn(count, rank, outputs, generator=g) / math.sqrt(rank)).to(dtype).to(dev)
+            self.scale = (0.5 + torch.rand(count, generator=g)).to(dev) if scale else None
+            starts = np.concatenate([[first], first + np.cumsum(lengths)])
+            self.starts = torch.tensor(starts, dtype=torch.int32, device=dev)
+            if which is None:
+                which = torch.randint(-1, count, (len(lengths),), generator=g).tolist()
+            self.which = torch.tensor(which, dtype=torch.int32, device=dev)
+            self.adapters = binding.Adapters(self.a, self.b, self.scale)
+            self.ids = owners(self.starts, self.which, tokens, count)
+        else:
+            self.starts = self.which = self.adapters = None
+            self.ids = np.full(tokens, -1)
+        self.used = torch.tensor(self.ids != -2, device=dev)
+        self.outside = self.used.logical_not()
+
+    def rows(self, i):
+        return torch.tensor(self.ids == i, device=self.x.device)
+
+    def factor(self, i):
+        return self.scale[i].double() if self.scale is not None else 1.0
+
+    def forward(self):
+        """(y, its magnitude, hidden, its magnitude)"""
+        x = self.x.double()
+        beta, step, c = weight_parts(self.weights)
+        y = x @ (beta + step * c)
+        mag = (x.abs() @ c.abs()) * step + x.abs().sum(1, keepdim=True) * beta.abs()
+        h = torch.zeros(self.tokens, max(self.rank, 1), dtype=torch.float64, device=x.device)
+        hm = torch.zeros_like(h)
+        for i in range(self.count):
+            r = self.rows(i)
+            h[r] = self.factor(i) * (x[r] @ self.a[i].double().T)
+            hm[r] = self.factor(i) * (x[r].abs() @ self.a[i].double().abs().T)
+            y[r] += h[r] @ self.b[i].double()
+            mag[r] += hm[r] @ self.b[i].double().abs()
+        return y, mag, h, hm
+
+    def backward(self, hidden, cp):
+        """dx, its magnitude, v's magnitude through it, then (da, magnitude), (db, magnitude)"""
+        dy = torch.where(self.used[:, None], self.dy.double(), 0.0)
+        beta, step, c = weight_parts(self.weights)
+        dx = dy @ (beta + step * c).T
+        mag = (dy.abs() * step) @ c.abs().T + (dy.abs() @ beta.abs())[:, None]
+        out = []
+        if self.count:
+            lo, st, codes = checkpoint_values(cp)
+            q, qm = lo + st * codes, st * (codes - 128).abs() + (lo + 128 * st).abs()
+            da, dam = torch.zeros_like(self.a, dtype=torch.float64), torch.zeros_like(self.a, dtype=torch.float64)
+            db, dbm = torch.zeros_like(self.b, dtype=torch.float64), torch.zeros_like(self.b, dtype=torch.float64)
+            for i in range(self.count):
+                r = self.rows(i)
+                v = self.factor(i) * (dy[r] @ self.b[i].double().T)
+                vm = self.factor(i) * (dy[r].abs() @ self.b[i].double().abs().T)
+                dx[r] += v @ self.a[i].double()
+                mag[r] += vm @ self.a[i].double().abs()
+                da[i], dam[i] = v.T @ q[:self.tokens][r], vm.T @ qm[:self.tokens][r]
+                db[i], dbm[i] = hidden[r].double().T @ dy[r], hidden[r].double().abs().T @ dy[r].abs()
+            out = [da, dam, db, dbm]
+        return [dx, mag] + out
+
+
+def close(got, want, tol, where=None):
+    got = got.double()
+    off = (got - want).abs() - tol
+    if where is not None:
+        off = off[where]
+    assert torch.isfinite(got if where is None else got[where]).all()
+    assert off.numel() == 0 or off.max() <= 0, f"beyond its tolerance by {off.max().item():.3g} (largest value {want.abs().max().item():.3g})"
+
+
+def check_forward(ctx, p, out=None, hidden=None):
+    hidden = torch.full((p.tokens, p.rank), 7.0, device=ctx.device) if hidden is None and p.count else hidden
+    out = torch.full((p.tokens, p.weights.n), 3.0, dtype=p.dtype, device=ctx.device) if out is None else out
+    y = ctx.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which, out=out, hidden=hidden)
+    ctx.zipml_sync()
+    ref, mag, h, hm = p.forward()
+    k = p.weights.m
+    # sums in fp32 over the depth, then the ranks; hidden's two 16-bit parts leave 2^-16 (bf16) of it
+    close(y, ref, half_step(p.dtype) * ref.abs() * 1.01 + (k + 2 * p.rank + 16) * 2.0**-23 * mag + 2.0**-16 * mag, p.used)
+    assert (y[p.outside] == 3.0).all()
+    if p.count:
+        close(hidden, h, (k + 8) * 2.0**-23 * hm, p.used)
+        assert (hidden[p.outside] == 7.0).all()
+    return y, hidden
+
+
+def check_backward(ctx, p, hidden=None):
+    hidden = torch.randn(p.tokens, p.rank, device=ctx.device) if hidden is None and p.count else hidden
+    cp = ctx.zipml_checkpoint_encode(p.x, group=p.group, seed=5) if p.count else None
+    out = torch.full((p.tokens, p.weights.m), 3.0, dtype=p.dtype, device=ctx.device)
+    dx, da, db = ctx.zipml_project_backward(p.weights, p.dy, adapters=p.adapters, starts=p.starts, which=p.which, hidden=hidden, checkpoint=cp, out=out)
+    ctx.zipml_sync()
+    ref = p.backward(hidden, cp)
+    n = p.weights.n
+    # dY step is rounded to fp16's 11 bits (2^-11; what lies 2^-28 below a row's largest to 2^-38 of that), v enters in two 16-bit parts
+    tops = (p.dy.double().abs() * p.weights.feat_step.double()).amax(1, keepdim=True)
+    low = 2.0**-38 * tops * 128 * n
+    close(dx, ref[0], half_step(p.dtype) * ref[0].abs() * 1.01 + (2.0**-11 + 2.0**-16 + (n + 2 * p.rank + 16) * 2.0**-23) * ref[1] + low, p.used)
+    assert (dx[p.outside] == 3.0).all()
+    if p.count:
+        # v in fp32 over the outputs; factors in two tf32 parts leave 2^-20; sums over the tokens
+        close(da, ref[2], (2.0**-20 + (n + p.tokens + 64) * 2.0**-23) * ref[3] + 1e-30)
+        close(db, ref[4], (2.0**-20 + (p.tokens + 64) * 2.0**-23) * ref[5] + 1e-30)
+    return dx, da, db
+
+
+# --- checkpoints ----------------------------------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("group", [32, 64, 128, 256])
+@pytest.mark.parametrize("m,n", [(1, 1), (3, 7), (2, 8), (5, 33), (4, 255), (3, 256), (2, 257), (33, 1000), (1, 4099)])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_checkpoint_is_the_stated_rounding(ctx, m, n, group, dtype):
+    g = torch.Generator().manual_seed(m * 1000 + n)
+    x = (torch.randn(m, n, generator=g) * torch.exp(2 * torch.randn(1, n, generator=g))).to(dtype)
+    seed = 0x1234567_89ABCDEF
+    cp = ctx.zipml_checkpoint_encode(x.to(ctx.device), group=group, seed=seed)
+    back = ctx.zipml_checkpoint_decode(cp, dtype=F32)
+    narrow = ctx.zipml_checkpoint_decode(cp, dtype=dtype)
+    ctx.zipml_sync()
+    codes, grids = plain_encode(x, group, seed)
+    assert (cp.codes[:, :n].cpu().numpy() == codes).all()
+    assert (cp.codes[:, n:] == 0).all()
+    assert (cp.grids.cpu().numpy() == grids).all()
+    lo, step, c = checkpoint_values(cp)
+    want = lo + step * c
+    close(back, want, 2.0**-24 * want.abs() + 2.0**-149)                        # one fused rounding
+    assert torch.equal(narrow, back.to(dtype))
+    # never further than an interval from the value
+    assert ((back.double() - x.double().to(ctx.device)).abs() <= step * (1 + 1e-5) + 2.0**-23 * want.abs()).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("offset,extra", [(1, 3), (0, 5), (8, 8)])
+def test_checkpoint_of_strided_rows(ctx, dtype, offset, extra):
+    wide = torch.randn(9, offset + 100 + extra, device=ctx.device).to(dtype)
+    x = wide[:, offset:offset + 100]
+    cp = ctx.zipml_checkpoint_encode(x, group=32, seed=3)
+    codes, grids = plain_encode(x, 32, 3)
+    out = torch.full((9, 100 + offset + extra), 5.0, device=ctx.device, dtype=dtype)
+    ctx.zipml_checkpoint_decode(cp, out=out[:, offset:offset + 100])
+    ctx.zipml_sync()
+    assert (cp.codes[:, :100].cpu().numpy() == codes).all() and (cp.grids.cpu().numpy() == grids).all()
+    assert torch.equal(out[:, offset:offset + 100], ctx.zipml_checkpoint_decode(cp, dtype=dtype))
+    assert (out[:, :offset] == 5).all() and (out[:, offset + 100:] == 5).all()
+
+
+@gpu
+def test_checkpoint_of_constant_tiny_and_large_groups(ctx):
+    x = torch.zeros(6, 64, device=ctx.device)
+    x[1] = -3.25
+    x[2, :32] = torch.linspace(0, 1e-38, 32)                                    # a range of subnormal steps
+    x[3] = torch.linspace(-1.6e38, 1.6e38, 64)
+    x[4, 5] = 1e30
+    x[5, ::2] = -0.0
+    cp = ctx.zipml_checkpoint_encode(x, group=32, seed=1)
+    back = ctx.zipml_checkpoint_decode(cp, dtype=F32)
+    ctx.zipml_sync()
+    codes, grids = plain_encode(x, 32, 1)
+    assert (cp.codes[:, :64].cpu().numpy() == codes).all() and (cp.grids.cpu().numpy() == grids).all()
+    assert (back[0] == 0).all() and (back[1] == -3.25).all() and (back[5] == 0).all()
+    assert ((back[2] - x[2]).abs() <= 1e-38).all()
+    assert ((back[3] - x[3]).abs() <= 3.2e38 / 255).all()
+    assert abs(back[4, 5].item() - 1e30) <= 1e24
+
+
+@gpu
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_checkpoint_reports_what_is_not_finite(ctx, bad):
+    x = torch.randn(40, 300, device=ctx.device)
+    x[17, 299] = bad
+    ctx.zipml_checkpoint_encode(x, group=64)
+    with pytest.raises(binding.ZipmlError) as e:
+        ctx.zipml_sync()
+    assert e.value.code == binding.ERR_NONFINITE
+    x[17, 299] = 3e38
+    x[17, 298] = -3e38                                                          # a range that fp32 does not hold
+    ctx.zipml_checkpoint_encode(x, group=64)
+    with pytest.raises(binding.ZipmlError) as e:
+        ctx.zipml_sync()
+    assert e.value.code == binding.ERR_NONFINITE
+    ctx.zipml_checkpoint_encode(x[:17], group=64)
+    ctx.zipml_sync()
+
+
+@gpu
+def test_checkpoint_is_unbiased(ctx):
+    x = torch.rand(1, 64, device=ctx.device)
+    n = 4000
+    rows = x.expand(n, 64).contiguous()
+    cp = ctx.zipml_checkpoint_encode(rows, group=64, seed=11)
+    mean = ctx.zipml_checkpoint_decode(cp, dtype=F32).double().mean(0)
+    step = cp.grids[0, 0, 1].double()
+    # variance of one draw at most step^2 / 4; five deviations of the mean, and the 2^-16 of an interval that the draws' grid costs
+    assert ((mean - x[0].double()).abs() <= step * (5 * 0.5 / math.sqrt(n) + 2.0**-16 + 1e-4)).all()
+
+
+@gpu
+def test_checkpoint_of_no_rows(ctx):
+    cp = ctx.zipml_checkpoint_encode(torch.empty(0, 40, device=ctx.device, dtype=BF16), group=32)
+    assert ctx.zipml_checkpoint_decode(cp).shape == (0, 40)
+    ctx.zipml_sync()
+
+
+# --- projection -----------------------------------------------------------------------------------------------------------------
+
+SHAPES = [
+    # tokens, inputs, outputs, bits, rank, adapters, lengths
+    (1, 64, 128, 8, 16, 2, [1]),
+    (1, 1000, 257, 4, 8, 3, [1]),
+    (5, 8, 1, 8, 1, 1, [2, 3]),
+    (7, 65, 40, 2, 3, 2, [0, 3, 0, 4]),
+    (16, 512, 1024, 6, 33, 4, [1] * 16),
+    (17, 300, 130, 3, 128, 2, [9, 8]),
+    (40, 129, 520, 5, 12, 40, [1] * 40),
+    (64, 2048, 384, 8, 64, 3, [30, 2, 32]),
+    (100, 777, 333, 1, 16, 5, [10, 20, 30, 40]),
+    (130, 1024, 2049, 4, 40, 6, [1, 128, 1]),
+    (300, 256, 1200, 7, 16, 7, [100, 57, 3, 140]),
+    (700, 520, 2600, 8, 8, 3, [256, 256, 188]),
+]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s[:6])))
+def test_projection(ctx, shape, dtype):
+    tokens, inputs, outputs, bits, rank, count, lengths = shape
+    check_forward(ctx, Problem(ctx, tokens, inputs, outputs, bits, dtype, rank, count, lengths, seed=tokens))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s[:6])))
+def test_projection_backward(ctx, shape, dtype):
+    tokens, inputs, outputs, bits, rank, count, lengths = shape
+    check_backward(ctx, Problem(ctx, tokens, inputs, outputs, bits, dtype, rank, count, lengths, seed=tokens, group=(32, 64, 128, 256)[tokens % 4]))
+
+
+@gpu
+@pytest.mark.parametrize("tokens", [1, 15, 16, 63, 65, 129, 257, 600])
+@pytest.mark.parametrize("bits", [2, 4, 8])
+def test_projection_alone(ctx, tokens, bits):
+    p = Problem(ctx, tokens, 320, 700, bits, BF16, 0, 0, [])
+    check_forward(ctx, p)
+    check_backward(ctx, p)
+
+
+@gpu
+@pytest.mark.parametrize("group", [32, 64, 128, 256])
+@pytest.mark.parametrize("inputs", [31, 128, 200, 1000])
+def test_gradients_of_every_group_size(ctx, inputs, group):
+    check_backward(ctx, Problem(ctx, 90, inputs, 96, 8, BF16, 16, 2, [30, 25, 35], which=[0, 1, 0], group=group))
+
+
+@gpu
+@pytest.mark.parametrize("which", [[-1, -1, -1], [0, 0, 0], [1, -1, 1], [2, 1, 0]])
+def test_who_uses_which_adapter(ctx, which):
+    p = Problem(ctx, 80, 200, 264, 8, F16, 8, 3, [20, 50, 10], which=which)
+    check_forward(ctx, p)
+    _, da, db = check_backward(ctx, p)
+    for i in range(3):                                                          # adapters that nobody uses have no gradient
+        if i not in which:
+            assert (da[i] == 0).all() and (db[i] == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("first,lengths", [(0, [10, 20]), (5, [3, 0, 40]), (0, [0, 0]), (69, [1])])
+def test_tokens_outside_the_requests_stay_as_they_were(ctx, first, lengths):
+    p = Problem(ctx, 70, 150, 200, 4, BF16, 16, 2, lengths, which=[i % 2 for i in range(len(lengths))], first=first)
+    p.x[p.outside] = float("nan")                                               # nor does anything in them reach the others
+    p.dy[p.outside] = float("inf")
+    check_forward(ctx, p)
+    p.x[p.outside] = 0.0                                                        # (the checkpoint reports what is not finite)
+    check_backward(ctx, p)
+
+
+@gpu
+@pytest.mark.parametrize("ldx,ldy", [(203, 301), (208, 300), (201, 304)])
+def test_strides_that_are_not_aligned(ctx, ldx, ldy):
+    p = Problem(ctx, 45, 200, 300, 8, BF16, 16, 3, [20, 25], ldx=ldx)
+    wide = torch.full((45, ldy), 3.0, dtype=BF16, device=ctx.device)
+    check_forward(ctx, p, out=wide[:, :300])
+    assert (wide[:, 300:] == 3.0).all()
+    p.dy = torch.randn(45, ldy, device=ctx.device).to(BF16)[:, :300]
+    check_backward(ctx, p)
+
+
+@gpu
+def test_bases_that_are_not_aligned(ctx):
+    p = Problem(ctx, 20, 64, 72, 8, F16, 8, 2, [20])
+    flat = torch.zeros(20 * 64 + 1, dtype=F16, device=ctx.device)
+    flat[1:] = p.x.reshape(-1)
+    p.x = flat[1:].view(20, 64)
+    out = torch.full((20 * 72 + 1,), 3.0, dtype=F16, device=ctx.device)[1:].view(20, 72)
+    check_forward(ctx, p, out=out)
+    flat = torch.zeros(20 * 72 + 1, dtype=F16, device=ctx.device)
+    flat[1:] = p.dy.reshape(-1)
+    p.dy = flat[1:].view(20, 72)
+    for name in ("a", "b"):                                                     # adapters that start between two 16-byte lines
+        t = getattr(p, name)
+        flat = torch.zeros(t.numel() + 1, dtype=F16, device=ctx.device)
+        flat[1:] = t.reshape(-1)
+        setattr(p, name, flat[1:].view(t.shape))
+    p.adapters = binding.Adapters(p.a, p.b, p.scale)
+    check_forward(ctx, p)
+    check_backward(ctx, p)
+
+
+@gpu
+def test_without_scales_and_without_hidden(ctx):
+    p = Problem(ctx, 33, 160, 136, 8, BF16, 4, 2, [13, 20], scale=False)
+    y, _ = check_forward(ctx, p)
+    again = ctx.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which)
+    assert torch.equal(again[p.used], y[p.used])
+
+
+@gpu
+def test_an_index_past_the_adapters_counts_as_none(ctx):
+    p = Problem(ctx, 30, 96, 64, 8, BF16, 4, 2, [10, 20], which=[1, 2])
+    y = ctx.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which)
+    with pytest.raises(binding.ZipmlError) as e:
+        ctx.zipml_sync()
+    assert e.value.code == binding.ERR_INVALID_ARG
+    p.which[1] = -1
+    assert torch.equal(y, ctx.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which))
+    ctx.zipml_sync()
+
+
+@gpu
+@pytest.mark.parametrize("tokens", [12, 200])
+def test_what_is_not_finite_stays_with_its_request(ctx, tokens):
+    p = Problem(ctx, tokens, 192, 256, 8, F16, 8, 2, [tokens // 2, tokens - tokens // 2], which=[0, 1])
+    y = ctx.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which)
+    p.x[1, 3] = float("inf")
+    p.x[2, 4] = float("nan")
+    got = ctx.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which)
+    ctx.zipml_sync()
+    rest = [t for t in range(tokens) if t not in (1, 2)]
+    assert torch.equal(got[rest], y[rest]) and not torch.isfinite(got[1]).any() and torch.isnan(got[2]).all()
+    p.x[1:3] = 0.5
+    y = ctx.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which)
+    p.b[0, 1, 7] = float("nan")
+    p.b[0, 2, 9] = float("-inf")
+    got = ctx.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which)
+    with pytest.raises(binding.ZipmlError) as e:
+        ctx.zipml_sync()
+    assert e.value.code == binding.ERR_NONFINITE
+    assert torch.equal(got[tokens // 2:], y[tokens // 2:])
+    p.b[0, 1:3] = 0.0
+    p.a[1, 0, 0] = float("nan")
+    got = ctx.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which)
+    ctx.zipml_sync()
+    assert torch.isfinite(got[:tokens // 2]).all()
+
+
+@gpu
+@pytest.mark.parametrize("factor", [2.0**-14, 2.0**13])
+def test_magnitudes_at_the_ends_of_fp16(ctx, factor):
+    """hidden and dY far from one: their 16-bit parts are taken after a power of two has brought each row into range."""
+    p = Problem(ctx, 50, 256, 128, 8, F16, 16, 2, [20, 30], which=[0, 1])
+    p.x *= factor / 8
+    p.dy *= factor / 8
+    p.b *= 1.0 / (8 * max(1.0, factor))
+    p.weights.feat_lo /= 4 * max(1.0, factor)
+    p.weights.feat_step /= 4 * max(1.0, factor)
+    y, mag, h, hm = p.forward()
+    hidden = torch.zeros(50, 16, device=ctx.device)
+    got = ctx.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which, hidden=hidden)
+    ctx.zipml_sync()
+    low = 2.0**-25                                                              # half a step of fp16's subnormal results
+    close(got, y, half_step(F16) * y.abs() * 1.01 + (256 + 48) * 2.0**-23 * mag + 2.0**-16 * mag + low)
+    cp = ctx.zipml_checkpoint_encode(p.x, group=32)
+    dx, da, db = ctx.zipml_project_backward(p.weights, p.dy, adapters=p.adapters, starts=p.starts, which=p.which, hidden=hidden, checkpoint=cp)
+    ctx.zipml_sync()
+    ref = p.backward(hidden, cp)
+    close(dx, ref[0], half_step(F16) * ref[0].abs() * 1.01 + (2.0**-11 + 2.0**-16 + 256 * 2.0**-23) * ref[1] + low)
+    close(da, ref[2], (2.0**-20 + 300 * 2.0**-23) * ref[3] + 1e-30)
+    close(db, ref[4], (2.0**-20 + 200 * 2.0**-23) * ref[5] + 1e-30)
+
+
+@gpu
+def test_no_tokens(ctx):
+    p = Problem(ctx, 4, 64, 80, 8, BF16, 8, 2, [4])
+    empty = p.x[:0]
+    assert ctx.zipml_project(p.weights, empty, adapters=p.adapters, starts=p.starts, which=p.which).shape == (0, 80)
+    cp = ctx.zipml_checkpoint_encode(empty, group=32)
+    dx, da, db = ctx.zipml_project_backward(p.weights, p.dy[:0], adapters=p.adapters, starts=p.starts, which=p.which,
+                                            hidden=torch.zeros(0, 8, device=ctx.device), checkpoint=cp)
+    ctx.zipml_sync()
+    assert dx.shape == (0, 64) and (da == 0).all() and (db == 0).all()
+
+
+@gpu
+def test_parts_of_the_backward_pass(ctx):
+    p = Problem(ctx, 60, 128, 192, 4, BF16, 8, 2, [30, 30], which=[1, 0])
+    dx, da, db = check_backward(ctx, p, hidden=torch.ones(60, 8, device=ctx.device))
+    cp = ctx.zipml_checkpoint_encode(p.x, group=p.group, seed=5)
+    kw = dict(adapters=p.adapters, starts=p.starts, which=p.which)
+    only = ctx.zipml_project_backward(p.weights, p.dy, checkpoint=cp, want_input=False, **kw)
+    assert only[0] is None and only[2] is None and torch.equal(only[1], da)
+    only = ctx.zipml_project_backward(p.weights, p.dy, hidden=torch.ones(60, 8, device=ctx.device), want_input=False, **kw)
+    assert only[0] is None and only[1] is None and torch.equal(only[2], db)
+    only = ctx.zipml_project_backward(p.weights, p.dy, **kw)
+    assert torch.equal(only[0], dx) and only[1] is None and only[2] is None
+    ctx.zipml_sync()
+
+
+@gpu
+def test_gradients_against_differences(ctx):
+    """The projection is linear in its input and in each factor: differences of any length give the gradient of sum(Y * dY)."""
+    p = Problem(ctx, 48, 120, 90, 8, F16, 8, 2, [18, 30], which=[0, 1])
+    hidden = torch.zeros(48, 8, device=ctx.device)
+    base = ctx.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which, hidden=hidden)
+    cp = ctx.zipml_checkpoint_encode(p.x, group=32, seed=2)
+    dx, da, db = ctx.zipml_project_backward(p.weights, p.dy, adapters=p.adapters, starts=p.starts, which=p.which, hidden=hidden, checkpoint=cp)
+    quantized = ctx.zipml_checkpoint_decode(cp, dtype=F32)
+    ctx.zipml_sync()
+
+    def loss(x, a, b):
+        y = ctx.zipml_project(p.weights, x, adapters=binding.Adapters(a, b, p.scale), starts=p.starts, which=p.which)
+        ctx.zipml_sync()
+        return (y.double() * p.dy.double()).sum().item()
+
+    at = (base.double() * p.dy.double()).sum().item()
+    rounding = half_step(F16) * (base.double().abs() * p.dy.double().abs()).sum().item()
+    step = torch.randn_like(p.x) * 4
+    after = loss(p.x + step, p.a, p.b)
+    moved = ((p.x + step).double() - p.x.double())
+    assert abs((after - at) - (moved * dx.double()).sum().item()) <= 12 * rounding
+    step = torch.zeros_like(p.b)
+    step[1] = torch.randn_like(p.b[1]) * 4
+    after = loss(p.x, p.a, p.b + step)
+    assert abs((after - at) - (((p.b + step).double() - p.b.double()) * db.double()).sum().item()) <= 12 * rounding
+    step = torch.zeros_like(p.a)
+    step[0] = torch.randn_like(p.a[0])
+    after = loss(p.x, p.a + step, p.b)
+    moved = (p.a + step).double() - p.a.double()
+    # the checkpoint's values stand in for x: the gradient is that of the same differences taken on them, so what the rounding of x adds is known
+    v = p.scale.double()[0] * (p.dy[:18].double() @ p.b[0].double().T)
+    error = ((v.T @ (quantized[:18].double() - p.x[:18].double())) * moved[0]).sum().item()
+    assert abs((after - at) - ((moved * da.double()).sum().item() - error)) <= 12 * rounding
+
+
+# --- how calls are made -----------------------------------------------------------------------------------------------------------
+
+@gpu
+def test_fine_tuning_steps_run_together(ctx):
+    """Encode, project, backward and an update, a few times over, as a training loop has them; each step's gradients are checked."""
+    p = Problem(ctx, 96, 256, 320, 4, BF16, 8, 2, [40, 30, 26], which=[0, 1, 0])
+    a, b = p.a.float(), p.b.float()
+    for step in range(3):
+        hidden = torch.zeros(96, 8, device=ctx.device)
+        p.a, p.b = a.to(BF16), b.to(BF16)
+        p.adapters = binding.Adapters(p.a, p.b, p.scale)
+        cp = ctx.zipml_checkpoint_encode(p.x, group=64, seed=step)
+        y = ctx.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which, hidden=hidden)
+        p.dy = (y.float() / y.numel()).to(BF16)
+        dx, da, db = ctx.zipml_project_backward(p.weights, p.dy, adapters=p.adapters, starts=p.starts, which=p.which, hidden=hidden, checkpoint=cp)
+        ctx.zipml_sync()
+        ref = p.backward(hidden, cp)
+        close(da, ref[2], (2.0**-20 + (320 + 96 + 64) * 2.0**-23) * ref[3] + 1e-30)
+        close(db, ref[4], (2.0**-20 + (96 + 64) * 2.0**-23) * ref[5] + 1e-30)
+        a -= 0.1 * da
+        b -= 0.1 * db
+
+
+@gpu
+@pytest.mark.parametrize("tokens", [3, 150])
+def test_results_do_not_change_from_call_to_call(ctx, tokens):
+    p = Problem(ctx, tokens, 700, 900, 8, BF16, 16, 2, [tokens])
+    first = check_forward(ctx, p) + check_backward(ctx, p, hidden=torch.ones(tokens, 16, device=ctx.device))
+    for _ in range(3):
+        again = check_forward(ctx, p) + check_backward(ctx, p, hidden=torch.ones(tokens, 16, device=ctx.device))
+        assert all(torch.equal(u, v) for u, v in zip(first, again))
+
+
+@gpu
+@pytest.mark.parametrize("tokens", [2, 130])
+def test_captured_calls_replay(ctx, tokens):
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream), binding.Context("cuda:0", stream=stream) as c:
+        p = Problem(c, tokens, 300, 280, 8, BF16, 8, 2, [tokens])
+        p.which[0] = 1
+        stream.synchronize()
+        y, hidden = torch.zeros(tokens, 280, dtype=BF16, device="cuda:0"), torch.zeros(tokens, 8, device="cuda:0")
+        dx, da, db = torch.zeros(tokens, 300, dtype=BF16, device="cuda:0"), torch.zeros(2, 8, 300, device="cuda:0"), torch.zeros(2, 8, 280, device="cuda:0")
+        cp = c.zipml_checkpoint_encode(p.x, group=64, seed=4)
+
+        def calls():
+            c.zipml_checkpoint_encode(p.x, group=64, seed=4, out=cp)
+            c.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which, out=y, hidden=hidden)
+            c.zipml_project_backward(p.weights, p.dy, adapters=p.adapters, starts=p.starts, which=p.which, hidden=hidden, checkpoint=cp, out=dx,
+                                     grad_a=da, grad_b=db)
+
+        calls()
+        stream.synchronize()
+        want = [t.clone() for t in (y, hidden, dx, da, db, cp.codes)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            calls()
+        # the context's workspace grows for a larger call: the recorded launches keep theirs
+        big = Problem(c, 2000, 300, 280, 8, BF16, 8, 2, [2000])
+        check_forward(c, big)
+        for t in (y, hidden, dx, da, db, cp.codes):
+            t.zero_()
+        graph.replay()
+        stream.synchronize()
+        c.zipml_sync()
+        assert all(torch.equal(u, v) for u, v in zip(want, (y, hidden, dx, da, db, cp.codes)))
+        # other inputs in the same places
+        p.x.copy_(torch.randn_like(p.x))
+        p.dy.copy_(torch.randn_like(p.dy))
+        graph.replay()
+        stream.synchronize()
+        got = [t.clone() for t in (y, hidden, dx, da, db, cp.codes)]
+        calls()
+        stream.synchronize()
+        assert all(torch.equal(u, v) for u, v in zip(got, (y, hidden, dx, da, db, cp.codes)))
+        del graph
+
+
+@gpu
+def test_capture_refuses_to_grow_the_workspace():
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream), binding.Context("cuda:0", stream=stream) as c:
+        p = Problem(c, 20, 64, 64, 8, BF16, 8, 2, [20])
+        out = torch.zeros(20, 64, dtype=BF16, device="cuda:0")
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            with pytest.raises(binding.ZipmlError) as e:
+                c.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which, out=out)
+            out += 1                                                            # (a graph of something)
+        assert e.value.code == binding.ERR_WORKSPACE
+        graph.replay()
+        stream.synchronize()
+        assert (out == 1).all()
+        del graph
+
+
+@gpu
+def test_refusals(ctx):
+    p = Problem(ctx, 10, 64, 64, 8, BF16, 8, 2, [10])
+    kw = dict(adapters=p.adapters, starts=p.starts, which=p.which)
+
+    def refused(code, call, *a, **k):
+        with pytest.raises(binding.ZipmlError) as e:
+            call(*a, **k)
+        assert e.value.code == code
+
+    launches = ctx.zipml_kernel_launches()
+    table = binding.Dataset(p.weights.plane1, p.weights.plane2, 64, 64, 4, binding.LEVELS_TABLE, p.weights.feat_lo, None,
+                            torch.zeros(64, 16, device=ctx.device))
+    refused(binding.ERR_UNSUPPORTED, ctx.zipml_project, table, p.x, **kw)
+    blocks = binding.Dataset(p.weights.plane1, p.weights.plane2, 64, 64, 8, binding.LEVELS_UNIFORM, p.weights.feat_lo, p.weights.feat_step, None,
+                             layout=binding.LAYOUT_COLUMN_BLOCKS)
+    refused(binding.ERR_UNSUPPORTED, ctx.zipml_project, blocks, p.x, **kw)
+    refused(binding.ERR_UNSUPPORTED, ctx.zipml_project, p.weights, p.x.float())
+    refused(binding.ERR_INVALID_ARG, ctx.zipml_project, p.weights, p.x.to(F16), **kw)
+    refused(binding.ERR_INVALID_ARG, ctx.zipml_project, p.weights, p.x, out=p.x, **kw)
+    big = binding.Adapters(torch.zeros(1, 129, 64, dtype=BF16, device=ctx.device), torch.zeros(1, 129, 64, dtype=BF16, device=ctx.device))
+    refused(binding.ERR_UNSUPPORTED, ctx.zipml_project, p.weights, p.x, adapters=big, starts=p.starts, which=p.which)
+    refused(binding.ERR_UNSUPPORTED, ctx.zipml_checkpoint_encode, p.x, group=48)
+    cp = ctx.zipml_checkpoint_encode(p.x[:9], group=32)
+    refused(binding.ERR_INVALID_ARG, ctx.zipml_project_backward, p.weights, p.dy, hidden=torch.zeros(10, 8, device=ctx.device), checkpoint=cp, **kw)
+    assert ctx.zipml_kernel_launches() == launches + 1
+    ctx.zipml_sync()
