@@ -14,7 +14,7 @@ namespace cg = cooperative_groups;
 // ---------------------------------------------------------------------------------------------
 // A CTA makes 128 features x NT tokens.  The features stand on the product's 128 rows and the tokens on its columns, so one
 // kernel serves from a token (16 columns, the codes' bytes are what counts) to thousands.  Per 64 of the depth:
-//   codes     a tensor copy brings the packed codes; eight warps turn them into 16-bit whole numbers code - 2^(cb-1), which are exact, and
+//   codes     a tensor copy brings the packed codes; groups of four warps, each with a stage of its own, turn them into 16-bit whole numbers code - 2^(cb-1), which are exact, and
 //             lay them out as the product's left operand.  Forward: a code row is one depth and holds the features (MN-major
 //             operand); backward: a code row is a feature (K-major).
 //   tokens    a tensor copy lays the right operand out itself.
@@ -27,52 +27,84 @@ namespace cg = cooperative_groups;
 // ---------------------------------------------------------------------------------------------
 constexpr int kProjRows = 128;                // features of a CTA
 constexpr int kProjDepth = 64;                // depth of a stage: 128 bytes of 16-bit operand
-constexpr int kUnpackWarps = 8;
-constexpr int kProjThreads = 32 * (4 + kUnpackWarps);
+constexpr int kGroups = 3;                    // groups of unpacking warps, each with every third stage
+constexpr int kGroupWarps = 4;
+constexpr int kGroupThreads = 32 * kGroupWarps;
+constexpr int kProjThreads = 32 * (4 + kGroups * kGroupWarps);
+constexpr int kMostSlots = 12;
 constexpr int kRankChunk = 32;                // ranks of an adapter stage: high parts in the first half of the depth, low ones in the second
-constexpr uint32_t kABytes = kProjRows * kProjDepth * 2;
+constexpr uint32_t kLeftBytes = kProjRows * kProjDepth * 2;
 
+// Slots of the rings.  The left operand's is the deepest: unpacking a stage takes some 1,000 cycles from its codes' arrival to its last
+// store, two products' worth, where a tensor copy of tokens only has L2's latency to cover.  A stage has one barrier that tells that both of
+// its operands are there and one that tells that its product is done (the issuing warp waits and commits once a stage: each took it over 100
+// cycles), in the left ring's order.  The groups' rings have a multiple of kGroups slots, so that a slot is always the same group's: a
+// barrier tells a phase from the one before it only, and a group that came to a slot whose last phase belonged to another could be a phase
+// early.
 template <int NT>
 struct ProjShape {
-    static constexpr int kStages = NT == 16 ? 6 : NT == 64 ? 5 : 4;
-    static constexpr int kCodeStages = NT == 256 ? 3 : NT == 128 ? 6 : 8;
-    static constexpr uint32_t kBBytes = NT * kProjDepth * 2;
-    static constexpr uint32_t kCodeBytes = kProjRows * kProjDepth;      // 8-bit codes; narrower ones fill a part
-    static constexpr uint32_t kRing = kStages * (kABytes + kBBytes) + kCodeStages * kCodeBytes;
+    static constexpr int kLeft = 2 * kGroups;
+    static constexpr int kRight = NT == 256 ? 3 : NT == 128 ? 4 : 6;
+    static constexpr uint32_t kRightBytes = NT * kProjDepth * 2;
+    static constexpr uint32_t kCodeRing = (NT == 256 ? 3 : NT == 128 ? 6 : NT == 64 ? 9 : 12) * kProjRows * kProjDepth;     // bytes for packed codes
+    static_assert(kRight >= kGroups && kRight <= kLeft && kLeft % kGroups == 0 && kMostSlots % kGroups == 0, "slots by group");
+    static constexpr uint32_t kRing = kLeft * kLeftBytes + kRight * kRightBytes + kCodeRing;
     static constexpr uint32_t kColumns = NT == 16 ? 32 : 2 * NT;        // tensor memory: codes' sums, then adapters'
+};
+
+struct ProjToken {                            // what the epilogue needs of a token
+    float row_scale, sum, hidden_scale;
+    int id;
 };
 
 template <int NT>
 struct ProjShared {
-    uint64_t tokens_full[8], codes_full[8], operand_full[8], empty[8], codes_empty[8], done, plan;
+    ProjToken token[NT];
+    uint64_t codes_full[kMostSlots], codes_empty[kMostSlots], full[2 * kGroups], empty[2 * kGroups];
+    uint64_t up_full[kGroups], up_empty[kGroups], codes_done, done, plan;
     uint32_t tmem;
     int gave_up;
     int entries;                              // adapters of this tile that fall to this CTA
     int entry_id[NT], entry_lo[NT], entry_n[NT];
-    int ids[NT];
-    float sum[NT], row_scale[NT], hidden_scale[NT];
 };
 
-// Sixteen packed codes as bytes.
+// A slot of a ring and the parity of its current turn.
+struct RingAt {
+    int slot = 0;
+    uint32_t turn = 0;
+    __device__ __forceinline__ void next(int by, int slots) {
+        slot += by;
+        if (slot >= slots) { slot -= slots; turn ^= 1u; }
+    }
+};
+
+// Sixteen packed codes, and as bytes.
 template <int CB>
-__device__ __forceinline__ void codes_to_bytes(const uint8_t* p, uint32_t (&w)[4]) {
+__device__ __forceinline__ void load_codes(const uint8_t* p, uint32_t (&w)[4]) {
     if constexpr (CB == 8) {
         const uint4 v = *reinterpret_cast<const uint4*>(p);
         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
     } else if constexpr (CB == 4) {
         const uint2 v = *reinterpret_cast<const uint2*>(p);
-        const uint32_t u[2] = {v.x, v.y};
+        w[0] = v.x; w[1] = v.y;
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+}
+template <int CB>
+__device__ __forceinline__ void codes_to_bytes(uint32_t (&w)[4]) {
+    if constexpr (CB == 4) {
+        const uint32_t u[2] = {w[0], w[1]};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t even = u[i] & 0x0F0F0F0Fu, odd = (u[i] >> 4) & 0x0F0F0F0Fu;
             w[2 * i] = __byte_perm(even, odd, 0x5140);
             w[2 * i + 1] = __byte_perm(even, odd, 0x7362);
         }
-    } else {
-        const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
+    } else if constexpr (CB == 2) {
         uint32_t t[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) t[k] = (v >> (2 * k)) & 0x03030303u;
+        for (int k = 0; k < 4; ++k) t[k] = (w[0] >> (2 * k)) & 0x03030303u;
         const uint32_t a0 = __byte_perm(t[0], t[1], 0x5140), a1 = __byte_perm(t[2], t[3], 0x5140);
         const uint32_t b0 = __byte_perm(t[0], t[1], 0x7362), b1 = __byte_perm(t[2], t[3], 0x7362);
         w[0] = __byte_perm(a0, a1, 0x5410); w[1] = __byte_perm(a0, a1, 0x7632);
@@ -106,17 +138,22 @@ __device__ __forceinline__ uint4 centred_chunk(uint32_t w0, uint32_t w1) {      
                       centred_pair<BF16, CB>(__byte_perm(w1, kTop, 0x4140)), centred_pair<BF16, CB>(__byte_perm(w1, kTop, 0x4342)));
 }
 
-// One stage's codes into the left operand, two units of 16 codes a thread.  Bank conflicts: eight lanes store 16 bytes each at a time;
+// One stage's codes into the left operand, four units of 16 codes a thread.  Bank conflicts: eight lanes store 16 bytes each at a time;
 // forward they hold one depth's 8 units, whose first halves would meet in pairs 8 KB apart, so the upper 64 features store their second
-// half first.
-template <bool BF16, int CB, bool BACK>
-__device__ __forceinline__ void unpack_stage(const uint8_t* codes, uint8_t* operand, int uid) {
+// half first.  The codes' slot is given back as soon as they are in registers; false where the left operand's wait gave up.
+template <bool BF16, int CB, bool BACK, class Free, class Wait>
+__device__ __forceinline__ bool unpack_stage(const uint8_t* codes, uint8_t* operand, int gid, Free free, Wait wait) {
+    constexpr int U = kProjRows * kProjDepth / 16 / kGroupThreads;
+    uint32_t w[U][4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int u = uid + i * 32 * kUnpackWarps;
-        uint32_t w[4];
-        codes_to_bytes<CB>(codes + u * 2 * CB, w);
-        const uint4 first = centred_chunk<BF16, CB>(w[0], w[1]), second = centred_chunk<BF16, CB>(w[2], w[3]);
+    for (int i = 0; i < U; ++i) load_codes<CB>(codes + (gid + i * kGroupThreads) * 2 * CB, w[i]);
+    free();
+    if (!wait()) return false;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int u = gid + i * kGroupThreads;
+        codes_to_bytes<CB>(w[i]);
+        const uint4 first = centred_chunk<BF16, CB>(w[i][0], w[i][1]), second = centred_chunk<BF16, CB>(w[i][2], w[i][3]);
         if constexpr (BACK) {
             const int row = u >> 2, chunk = 2 * (u & 3);                        // 16 of the depth of one feature
             uint8_t* p = operand + row * 128;
@@ -124,12 +161,13 @@ __device__ __forceinline__ void unpack_stage(const uint8_t* codes, uint8_t* oper
             *reinterpret_cast<uint4*>(p + (((chunk + 1) ^ (row & 7)) << 4)) = second;
         } else {
             const int k = u >> 3, f16 = u & 7, chunk = 2 * (f16 & 3);           // 16 features of one depth
-            uint8_t* p = operand + (f16 >> 2) * (kABytes / 2) + k * 128;
+            uint8_t* p = operand + (f16 >> 2) * (kLeftBytes / 2) + k * 128;
             const bool swap = f16 >= 4;
             *reinterpret_cast<uint4*>(p + (((chunk + swap) ^ (k & 7)) << 4)) = swap ? second : first;
             *reinterpret_cast<uint4*>(p + (((chunk + !swap) ^ (k & 7)) << 4)) = swap ? first : second;
         }
     }
+    return true;
 }
 
 // A 16-bit pair with what is not finite replaced by zero.
@@ -143,13 +181,13 @@ template <int NT, bool BACK, bool BF16>
 __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a, const __grid_constant__ CUtensorMap tokens_map,
                                                                   const __grid_constant__ CUtensorMap codes_map) {
     using Shape = ProjShape<NT>;
-    constexpr int S = Shape::kStages, CS = Shape::kCodeStages;
+    constexpr int L = Shape::kLeft, R = Shape::kRight;
     extern __shared__ uint8_t raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     ProjShared<NT>& sh = *reinterpret_cast<ProjShared<NT>*>(ring + Shape::kRing);
-    uint8_t* const left = ring;                                       // S x 16 KB
-    uint8_t* const right = ring + S * kABytes;
-    uint8_t* const packed = right + S * Shape::kBBytes;
+    uint8_t* const left = ring;
+    uint8_t* const right = ring + L * kLeftBytes;
+    uint8_t* const packed = right + R * Shape::kRightBytes;
     cg::cluster_group cluster = cg::this_cluster();
     const int crank = (int)cluster.block_rank(), cranks = (int)cluster.num_blocks();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -160,16 +198,24 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
     const int all_steps = (a.depth + kProjDepth - 1) / kProjDepth, per = (all_steps + cranks - 1) / cranks;
     const int step0 = min(crank * per, all_steps), steps = min(per, all_steps - step0);
     const int cb = a.bits;
+    const uint32_t code_bytes = (uint32_t)(kProjRows * kProjDepth / 8 * cb);
+    const int code_slots = min(kMostSlots, (int)(Shape::kCodeRing / code_bytes) / kGroups * kGroups);
     volatile int* gave_up = &sh.gave_up;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 8; ++i) {
-            mbar_init(&sh.tokens_full[i], 1);
+        for (int i = 0; i < kMostSlots; ++i) {
             mbar_init(&sh.codes_full[i], 1);
-            mbar_init(&sh.operand_full[i], kUnpackWarps);
-            mbar_init(&sh.empty[i], 1);
-            mbar_init(&sh.codes_empty[i], kUnpackWarps);
+            mbar_init(&sh.codes_empty[i], kGroupWarps);
         }
+        for (int i = 0; i < L; ++i) {
+            mbar_init(&sh.full[i], 1 + kGroupWarps);                       // the tokens' copy and the unpacking warps
+            mbar_init(&sh.empty[i], 1);
+        }
+        for (int i = 0; i < kGroups; ++i) {
+            mbar_init(&sh.up_full[i], kGroupWarps);
+            mbar_init(&sh.up_empty[i], 1);
+        }
+        mbar_init(&sh.codes_done, 1);
         mbar_init(&sh.done, 1);
         mbar_init(&sh.plan, 32);
         sh.gave_up = 0;
@@ -189,30 +235,33 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
         if (lane == 0) {
             if (a.early & 2) asm volatile("griddepcontrol.wait;" ::: "memory");
             int s = 0;
-            for (; s < steps; ++s) {
-                const int st = s % S;
-                if (s >= S && !tc_wait(&sh.empty[st], (s / S - 1) & 1, gave_up, a.status, 93)) break;
-                mbar_arrive_expect_tx(&sh.tokens_full[st], Shape::kBBytes);
-                tc_copy_2d(smem_u32(right + st * Shape::kBBytes), &tokens_map, (step0 + s) * kProjDepth, (int)t0, &sh.tokens_full[st]);
+            RingAt at;
+            RingAt stage, ahead;                                           // stage s, and s - R, whose place it takes
+            for (; s < steps; ++s, at.next(1, R), stage.next(1, L)) {
+                if (s >= R) {
+                    if (!tc_wait(&sh.empty[ahead.slot], ahead.turn, gave_up, a.status, 93)) break;
+                    ahead.next(1, L);
+                }
+                mbar_arrive_expect_tx(&sh.full[stage.slot], Shape::kRightBytes);
+                tc_copy_2d(smem_u32(right + at.slot * Shape::kRightBytes), &tokens_map, (step0 + s) * kProjDepth, (int)t0, &sh.full[stage.slot]);
             }
-            if (s < steps)
-                for (int i = max(0, s - S); i < s; ++i) tc_drain(&sh.tokens_full[i % S], (i / S) & 1);
+            if (s < steps)                                                 // (its stages' barriers want the unpacking warps too: they are waited for a while)
+                for (int i = max(0, s - R); i < s; ++i) tc_drain(&sh.full[i % L], (i / L) & 1);
         }
     } else if (warp == 2) {
         // the packed codes
         if (lane == 0) {
-            const uint32_t bytes = (uint32_t)(kProjRows * kProjDepth * cb / 8);
             int s = 0;
-            for (; s < steps; ++s) {
-                const int st = s % CS;
-                if (s >= CS && !tc_wait(&sh.codes_empty[st], (s / CS - 1) & 1, gave_up, a.status, 94)) break;
-                mbar_arrive_expect_tx(&sh.codes_full[st], bytes);
+            RingAt at;
+            for (; s < steps; ++s, at.next(1, code_slots)) {
+                if (s >= code_slots && !tc_wait(&sh.codes_empty[at.slot], at.turn ^ 1u, gave_up, a.status, 94)) break;
+                mbar_arrive_expect_tx(&sh.codes_full[at.slot], code_bytes);
                 const int depth = (step0 + s) * kProjDepth;
-                if (BACK) tc_copy_2d(smem_u32(packed + st * Shape::kCodeBytes), &codes_map, depth * cb / 8, f0, &sh.codes_full[st]);
-                else tc_copy_2d(smem_u32(packed + st * Shape::kCodeBytes), &codes_map, f0 / 8 * cb, depth, &sh.codes_full[st]);
+                if (BACK) tc_copy_2d(smem_u32(packed + at.slot * code_bytes), &codes_map, depth / 8 * cb, f0, &sh.codes_full[at.slot]);
+                else tc_copy_2d(smem_u32(packed + at.slot * code_bytes), &codes_map, f0 / 8 * cb, depth, &sh.codes_full[at.slot]);
             }
             if (s < steps)
-                for (int i = max(0, s - CS); i < s; ++i) tc_drain(&sh.codes_full[i % CS], (i / CS) & 1);
+                for (int i = max(0, s - code_slots); i < s; ++i) tc_drain(&sh.codes_full[i % code_slots], (i / code_slots) & 1);
         }
     } else if (warp == 3) {
         // what the first stage has found out about the tokens, and the adapters they need: each with the window of its tokens
@@ -223,13 +272,14 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
         for (int i = 0; i < PER; ++i) {
             const int t = lane + 32 * i;
             int id = kNoRequest;
+            ProjToken tok{1.0f, 0.0f, 1.0f, kNoRequest};
             if (t < NT && t0 + t < a.tokens) {
-                id = a.ids[t0 + t];
-                sh.sum[t] = a.sum[t0 + t];
-                sh.row_scale[t] = a.row_scale ? a.row_scale[t0 + t] : 1.0f;
-                sh.hidden_scale[t] = a.up && id >= 0 ? a.hidden_scale[t0 + t] : 0.0f;
+                tok.id = id = a.ids[t0 + t];
+                tok.sum = a.sum[t0 + t];
+                if (a.row_scale) tok.row_scale = a.row_scale[t0 + t];
+                if (a.up && id >= 0) tok.hidden_scale = a.hidden_scale[t0 + t];
             }
-            if (t < NT) sh.ids[t] = id;
+            if (t < NT) sh.token[t] = tok;
             mine[i] = chunks > 0 ? id : -1;
         }
         int found = 0, entries = 0;
@@ -268,67 +318,77 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
         __syncwarp();
         mbar_arrive(&sh.plan);
     } else if (warp == 1) {
-        // the products
-        if (lane == 0) {
-            bool ok = true;
-            int s = 0;
-            const uint32_t kind = tc_kind(BF16, !BACK, NT);
-            for (; s < steps; ++s) {
-                const int st = s % S;
-                ok = tc_wait(&sh.tokens_full[st], (s / S) & 1, gave_up, a.status, 95) && tc_wait(&sh.operand_full[st], (s / S) & 1, gave_up, a.status, 96);
+        // the products: the warp waits as a whole, one lane issues
+        bool ok = true;
+        RingAt la, ra;
+        const uint32_t kind = tc_kind(BF16, !BACK, NT);
+        // (operands by their first slot: an address in steps of 16 bytes is the description's lowest field)
+        const uint64_t left_at = BACK ? tc_operand(smem_u32(left), 16, 1024) : tc_operand(smem_u32(left), kLeftBytes / 2, 1024);
+        const uint64_t right_at = tc_operand(smem_u32(right), 16, 1024);
+        for (int s = 0; s < steps; ++s, la.next(1, L), ra.next(1, R)) {
+            ok = __all_sync(0xffffffffu, tc_wait(&sh.full[la.slot], la.turn, gave_up, a.status, 95));
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t lp = left_at + (uint32_t)la.slot * (kLeftBytes / 16), rp = right_at + (uint32_t)ra.slot * (Shape::kRightBytes / 16);
+            if (tc_elect()) {
+#pragma unroll
+                for (int k = 0; k < kProjDepth / 16; ++k) tc_mma(tmem, lp + k * (BACK ? 2 : 128), rp + k * 2, kind, s > 0 || k > 0);
+                tc_commit(&sh.empty[la.slot]);
+            }
+            __syncwarp();
+        }
+        if (tc_elect()) tc_commit(&sh.codes_done);
+        __syncwarp();
+        if (ok && chunks > 0) ok = __all_sync(0xffffffffu, tc_wait(&sh.plan, 0, gave_up, a.status, 97));
+        if (ok && chunks > 0) {
+            const int count = sh.entries * chunks;
+            const uint64_t up_at = tc_operand(smem_u32(left), kLeftBytes / 2, 1024);
+            for (int j = 0; j < count; ++j) {
+                const int slot = j % kGroups, e = j / chunks, c = j % chunks;
+                ok = __all_sync(0xffffffffu, tc_wait(&sh.up_full[slot], (j / kGroups) & 1, gave_up, a.status, 98));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t la = smem_u32(left + st * kABytes), ra = smem_u32(right + st * Shape::kBBytes);
-#pragma unroll
-                for (int k = 0; k < kProjDepth / 16; ++k) {
-                    const uint64_t da = BACK ? tc_operand(la + k * 32, 16, 1024) : tc_operand(la + k * 2048, kABytes / 2, 1024);
-                    tc_mma(tmem, da, tc_operand(ra + k * 32, 16, 1024), kind, s > 0 || k > 0);
+                const int lo = sh.entry_lo[e];
+                const uint64_t lp = up_at + (uint32_t)slot * (kLeftBytes / 16), rp = right_at + (uint32_t)slot * (Shape::kRightBytes / 16) + (uint32_t)lo * 8;
+                const uint32_t up_kind = tc_kind(BACK ? a.out_bf16 != 0 : BF16, true, sh.entry_n[e]);
+                const int ks = (min(kRankChunk, a.rank - c * kRankChunk) + 15) / 16;
+                if (tc_elect()) {
+                    for (int part = 0; part < 2; ++part)
+                        for (int k = 0; k < ks; ++k)
+                            tc_mma(tmem + Shape::kColumns / 2 + lo, lp + k * 128, rp + part * 4 + k * 2, up_kind, j > 0 || part > 0 || k > 0);
+                    tc_commit(&sh.up_empty[slot]);
                 }
-                tc_commit(&sh.empty[st]);
+                __syncwarp();
             }
-            if (ok && chunks > 0 && tc_wait(&sh.plan, 0, gave_up, a.status, 97)) {
-                const int entries = sh.entries;
-                for (int e = 0; ok && e < entries; ++e)
-                    for (int c = 0; c < chunks; ++c, ++s) {
-                        const int st = s % S;
-                        ok = tc_wait(&sh.operand_full[st], (s / S) & 1, gave_up, a.status, 98);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const int lo = sh.entry_lo[e];
-                        const uint32_t la = smem_u32(left + st * kABytes), ra = smem_u32(right + st * Shape::kBBytes) + lo * 128;
-                        const uint32_t up_kind = tc_kind(BACK ? a.out_bf16 != 0 : BF16, true, sh.entry_n[e]);
-                        const int ks = (min(kRankChunk, a.rank - c * kRankChunk) + 15) / 16;
-                        for (int part = 0; part < 2; ++part)
-                            for (int k = 0; k < ks; ++k)
-                                tc_mma(tmem + Shape::kColumns / 2 + lo, tc_operand(la + k * 2048, kABytes / 2, 1024),
-                                       tc_operand(ra + part * 64 + k * 32, 16, 1024), up_kind, e > 0 || c > 0 || part > 0 || k > 0);
-                        tc_commit(&sh.empty[st]);
-                    }
-            }
+        }
+        if (tc_elect()) {
             tc_commit(&sh.done);
             if (!ok) tc_drain(&sh.done, 0);
         }
+        __syncwarp();
     } else {
-        const int uid = threadIdx.x - 128;
-        int s = 0;
+        const int group = (warp - 4) / kGroupWarps, gid = (threadIdx.x - 128) % kGroupThreads;
+        int s = group;
         bool ok = true;
-        for (; s < steps; ++s) {
-            const int st = s % S, cs = s % CS;
-            ok = tc_wait(&sh.codes_full[cs], (s / CS) & 1, gave_up, a.status, 99);
-            if (ok && s >= S) ok = tc_wait(&sh.empty[st], (s / S - 1) & 1, gave_up, a.status, 100);
-            ok = __all_sync(0xffffffffu, ok);                          // (a warp gives up as a whole)
+        RingAt ca, la;
+        ca.next(group, code_slots); la.next(group, L);
+        for (; s < steps; s += kGroups, ca.next(kGroups, code_slots), la.next(kGroups, L)) {
+            ok = __all_sync(0xffffffffu, tc_wait(&sh.codes_full[ca.slot], ca.turn, gave_up, a.status, 99));       // (a warp gives up as a whole)
             if (!ok) break;
-            const uint8_t* src = packed + cs * Shape::kCodeBytes;
-            uint8_t* dst = left + st * kABytes;
-            if (cb == 8) unpack_stage<BF16, 8, BACK>(src, dst, uid);
-            else if (cb == 4) unpack_stage<BF16, 4, BACK>(src, dst, uid);
-            else unpack_stage<BF16, 2, BACK>(src, dst, uid);
+            const uint8_t* src = packed + ca.slot * code_bytes;
+            uint8_t* dst = left + la.slot * kLeftBytes;
+            const auto free = [&] {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.codes_empty[ca.slot]);
+            };
+            const auto wait = [&] { return s < L || __all_sync(0xffffffffu, tc_wait(&sh.empty[la.slot], la.turn ^ 1u, gave_up, a.status, 100)); };
+            if (cb == 8) ok = unpack_stage<BF16, 8, BACK>(src, dst, gid, free, wait);
+            else if (cb == 4) ok = unpack_stage<BF16, 4, BACK>(src, dst, gid, free, wait);
+            else ok = unpack_stage<BF16, 2, BACK>(src, dst, gid, free, wait);
+            if (!ok) break;
             tc_publish();
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(&sh.operand_full[st]);
-                mbar_arrive(&sh.codes_empty[cs]);
-            }
+            if (lane == 0) mbar_arrive(&sh.full[la.slot]);
         }
         if (ok) ok = __all_sync(0xffffffffu, tc_wait(&sh.plan, 0, gave_up, a.status, 101));
         if (ok && chunks > 0) {
@@ -337,63 +397,95 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             const uint32_t exponent = bf16 ? 0x7f80u : 0x7c00u;
             const uint16_t* up = reinterpret_cast<const uint16_t*>(a.up);
             const bool wide = ((reinterpret_cast<uintptr_t>(up) | (uintptr_t)((int64_t)a.features * 2)) & 15) == 0;
+            const bool wide_h = ((reinterpret_cast<uintptr_t>(a.hidden) | (uintptr_t)(a.rank * 4)) & 15) == 0;
             const int entries = sh.entries;
             bool bad = false;
-            for (int e = 0; ok && e < entries; ++e)
-                for (int c = 0; c < chunks; ++c, ++s) {
-                    const int st = s % S, id = sh.entry_id[e];
-                    if (s >= S) ok = __all_sync(0xffffffffu, tc_wait(&sh.empty[st], (s / S - 1) & 1, gave_up, a.status, 102));
-                    if (!ok) break;
-                    uint8_t* dst = left + st * kABytes;
-                    const int rows = min(kRankChunk, a.rank - c * kRankChunk), padded = (rows + 15) & ~15;
-                    for (int u = uid; u < padded * 16; u += 32 * kUnpackWarps) {
-                        const int k = u >> 4, chunk = u & 15, f = f0 + chunk * 8;
-                        uint4 w = make_uint4(0, 0, 0, 0);
-                        if (k < rows) w = load8_16(up + ((int64_t)id * a.rank + c * kRankChunk + k) * a.features + f, min(max(a.features - f, 0), 8), wide);
-                        w.x = finite_pair(w.x, exponent, bad); w.y = finite_pair(w.y, exponent, bad);
-                        w.z = finite_pair(w.z, exponent, bad); w.w = finite_pair(w.w, exponent, bad);
-                        *reinterpret_cast<uint4*>(dst + (chunk >> 3) * (kABytes / 2) + k * 128 + (((chunk & 7) ^ (k & 7)) << 4)) = w;
-                    }
-                    uint8_t* tok = right + st * Shape::kBBytes;
-                    const int lo = sh.entry_lo[e], n = sh.entry_n[e], per_row = padded >> 3;
-                    for (int u = uid; u < n * per_row; u += 32 * kUnpackWarps) {
-                        const int t = lo + u / per_row, chunk = u % per_row;
-                        float v[8] = {};
-                        if (sh.ids[t] == id) {
-                            const float inv = 1.0f / sh.hidden_scale[t];               // (a power of two)
-                            const float* h = a.hidden + (t0 + t) * a.rank + c * kRankChunk + chunk * 8;
+            // Stages again, each group with a slot of its own.  An adapter's rows are on their way before the slot is free.
+            for (int j = group; ok && j < entries * chunks; j += kGroups) {
+                const int e = j / chunks, c = j % chunks, id = sh.entry_id[e];
+                const int rows = min(kRankChunk, a.rank - c * kRankChunk), padded = (rows + 15) & ~15;
+                constexpr int U = kRankChunk * 16 / kGroupThreads;
+                uint4 w[U];
 #pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                if (chunk * 8 + i < rows) v[i] = h[i] * inv;
+                for (int i = 0; i < U; ++i) {
+                    const int u = gid + i * kGroupThreads, k = u >> 4, f = f0 + (u & 15) * 8;
+                    w[i] = make_uint4(0, 0, 0, 0);
+                    if (k < rows) w[i] = load8_16(up + ((int64_t)id * a.rank + c * kRankChunk + k) * a.features + f, min(max(a.features - f, 0), 8), wide);
+                }
+                const int lo = sh.entry_lo[e], n = sh.entry_n[e], per_row = padded >> 3, units = n * per_row;
+                constexpr int V = 4;                                       // units of 8 ranks of a token, on their way together
+                float v[V][8];
+                const auto load = [&](int from) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const int u = from + gid + i * kGroupThreads, t = lo + (per_row == 2 ? u >> 1 : u >> 2), chunk = u & (per_row - 1);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[i][k] = 0.0f;
+                        if (u < units && sh.token[t].id == id) {
+                            const float inv = 1.0f / sh.token[t].hidden_scale;     // (a power of two)
+                            const float* h = a.hidden + (t0 + t) * a.rank + c * kRankChunk + chunk * 8;
+                            if (wide_h && chunk * 8 + 8 <= rows) {
+                                const float4 x = *reinterpret_cast<const float4*>(h), y = *reinterpret_cast<const float4*>(h + 4);
+                                v[i][0] = x.x * inv; v[i][1] = x.y * inv; v[i][2] = x.z * inv; v[i][3] = x.w * inv;
+                                v[i][4] = y.x * inv; v[i][5] = y.y * inv; v[i][6] = y.z * inv; v[i][7] = y.w * inv;
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < 8; ++k)
+                                    if (chunk * 8 + k < rows) v[i][k] = h[k] * inv;
+                            }
                         }
+                    }
+                };
+                load(0);
+                ok = j < kGroups ? tc_wait(&sh.codes_done, 0, gave_up, a.status, 102)
+                                 : tc_wait(&sh.up_empty[group], (j / kGroups - 1) & 1, gave_up, a.status, 105);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                uint8_t* dst = left + group * kLeftBytes;
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    const int u = gid + i * kGroupThreads, k = u >> 4, chunk = u & 15;
+                    if (k >= padded) continue;
+                    w[i].x = finite_pair(w[i].x, exponent, bad); w[i].y = finite_pair(w[i].y, exponent, bad);
+                    w[i].z = finite_pair(w[i].z, exponent, bad); w[i].w = finite_pair(w[i].w, exponent, bad);
+                    *reinterpret_cast<uint4*>(dst + (chunk >> 3) * (kLeftBytes / 2) + k * 128 + (((chunk & 7) ^ (k & 7)) << 4)) = w[i];
+                }
+                uint8_t* tok = right + group * Shape::kRightBytes;
+                for (int from = 0; from < units; from += V * kGroupThreads) {
+                    if (from > 0) load(from);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const int u = from + gid + i * kGroupThreads, t = lo + (per_row == 2 ? u >> 1 : u >> 2), chunk = u & (per_row - 1);
+                        if (u >= units) continue;
                         uint32_t high[4], low[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
+                        for (int k = 0; k < 4; ++k) {
                             if (bf16) {
-                                high[i] = pack_pair<__nv_bfloat16>(v[2 * i], v[2 * i + 1]);
-                                const float2 f = unpack_pair<__nv_bfloat16>(high[i]);
-                                low[i] = pack_pair<__nv_bfloat16>(v[2 * i] - f.x, v[2 * i + 1] - f.y);
+                                high[k] = pack_pair<__nv_bfloat16>(v[i][2 * k], v[i][2 * k + 1]);
+                                const float2 f = unpack_pair<__nv_bfloat16>(high[k]);
+                                low[k] = pack_pair<__nv_bfloat16>(v[i][2 * k] - f.x, v[i][2 * k + 1] - f.y);
                             } else {
-                                high[i] = pack_pair<__half>(v[2 * i], v[2 * i + 1]);
-                                const float2 f = unpack_pair<__half>(high[i]);
-                                low[i] = pack_pair<__half>(v[2 * i] - f.x, v[2 * i + 1] - f.y);
+                                high[k] = pack_pair<__half>(v[i][2 * k], v[i][2 * k + 1]);
+                                const float2 f = unpack_pair<__half>(high[k]);
+                                low[k] = pack_pair<__half>(v[i][2 * k] - f.x, v[i][2 * k + 1] - f.y);
                             }
                         }
                         uint8_t* p = tok + t * 128;
                         *reinterpret_cast<uint4*>(p + ((chunk ^ (t & 7)) << 4)) = make_uint4(high[0], high[1], high[2], high[3]);
                         *reinterpret_cast<uint4*>(p + (((chunk + 4) ^ (t & 7)) << 4)) = make_uint4(low[0], low[1], low[2], low[3]);
                     }
-                    tc_publish();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.operand_full[st]);
                 }
+                tc_publish();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.up_full[group]);
+            }
             if (bad) set_status(a.status, ZIPML_ERR_NONFINITE, 103);
         }
         if (ok) ok = __all_sync(0xffffffffu, tc_wait(&sh.done, 0, gave_up, a.status, 104));
         if (ok) {
             tc_fence_after();
-            // two warps on each 32 rows of tensor memory, every other 16 tokens each
-            const int quarter = warp & 3, half = (warp - 4) >> 2;
+            // a group's warps take 32 rows of tensor memory each, the groups every third 16 tokens
+            const int quarter = warp & 3;
             const int row = quarter * 32 + lane, f = f0 + row;
             const bool in = f < a.features;
             float alpha = 1.0f, beta = 1.0f;
@@ -401,26 +493,43 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 alpha = a.step[f];
                 beta = fmaf(a.center, alpha, a.lo[f]);
             }
-            if (crank != 0) beta = 0.0f;
             const bool have_up = chunks > 0 && sh.entries > 0;
+            // A whole tile's rows pass through shared memory on their way out, so that a thread stores 16 bytes of a token's row.
             float* join = reinterpret_cast<float*>(ring);
-            for (int c = half; c < NT / 16; c += 2) {
+            uint16_t* stage = reinterpret_cast<uint16_t*>(ring) + group * 2 * 16 * kProjRows;
+            const bool wide_out = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * 2)) & 15) == 0;
+            for (int c = group; c < NT / 16; c += kGroups) {
                 uint32_t v[16], w[16];
                 if (steps > 0) tc_load16(tmem + ((uint32_t)(quarter * 32) << 16) + c * 16, v);
                 if (have_up) tc_load16(tmem + ((uint32_t)(quarter * 32) << 16) + Shape::kColumns / 2 + c * 16, w);
                 tc_load_wait();
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int t = c * 16 + i, id = sh.ids[t];
-                    if (id == kNoRequest) continue;
-                    float y = beta != 0.0f ? beta * sh.sum[t] : 0.0f;
-                    if (steps > 0) y = fmaf(alpha * sh.row_scale[t], __uint_as_float(v[i]), y);
-                    if (have_up && id >= 0) y = fmaf(sh.hidden_scale[t], __uint_as_float(w[i]), y);
-                    if (cranks > 1) join[t * kProjRows + row] = y;
-                    else if (in) {
-                        if (a.out_bf16) reinterpret_cast<__nv_bfloat16*>(a.out)[(t0 + t) * a.ldo + f] = __float2bfloat16_rn(y);
-                        else reinterpret_cast<__half*>(a.out)[(t0 + t) * a.ldo + f] = __float2half_rn(y);
+                    const ProjToken tok = sh.token[c * 16 + i];
+                    float y = crank == 0 ? beta * tok.sum : 0.0f;
+                    if (steps > 0) y = fmaf(alpha * tok.row_scale, __uint_as_float(v[i]), y);
+                    if (have_up && tok.id >= 0) y = fmaf(tok.hidden_scale, __uint_as_float(w[i]), y);
+                    if (cranks > 1) join[(c * 16 + i) * kProjRows + row] = y;
+                    else stage[i * kProjRows + row] = a.out_bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(y)) : __half_as_ushort(__float2half_rn(y));
+                }
+                if (cranks == 1) {
+                    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(kGroupThreads) : "memory");
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int u = gid + i * kGroupThreads, t = c * 16 + (u >> 4), at = f0 + (u & 15) * 8;
+                        if (sh.token[t].id == kNoRequest || at >= a.features) continue;
+                        const uint4 y = *reinterpret_cast<const uint4*>(stage + (u >> 4) * kProjRows + (u & 15) * 8);
+                        uint16_t* p = reinterpret_cast<uint16_t*>(a.out) + (t0 + t) * a.ldo + at;
+                        if (wide_out && at + 8 <= a.features) *reinterpret_cast<uint4*>(p) = y;
+                        else {
+                            const uint32_t e[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                if (at + k < a.features) p[k] = (uint16_t)(e[k >> 1] >> (16 * (k & 1)));
+                        }
                     }
+                    // (two buffers in turn: the next barrier tells that this one has been read)
+                    stage = reinterpret_cast<uint16_t*>(ring) + (group * 2 + (stage == reinterpret_cast<uint16_t*>(ring) + group * 2 * 16 * kProjRows)) * 16 * kProjRows;
                 }
             }
             tc_fence_before();
@@ -435,7 +544,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
         cluster.sync();
         const float* join = reinterpret_cast<const float*>(ring);
         for (int t = crank + cranks * warp; t < NT; t += cranks * (kProjThreads / 32)) {
-            if (sh.ids[t] == kNoRequest) continue;
+            if (sh.token[t].id == kNoRequest) continue;
             float y[4] = {};
             for (int c = 0; c < cranks; ++c) {
                 const float* p = cluster.map_shared_rank(join, c) + t * kProjRows;

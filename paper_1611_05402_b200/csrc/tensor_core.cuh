@@ -55,6 +55,13 @@ __device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint3
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"((uint32_t)accumulate) : "memory");
 }
+// One lane of a converged warp, chosen so that the compiler sees a uniform branch: what a matrix instruction takes then stays in uniform
+// registers.  (An `if (lane == 0)` around the loop cost some 100 cycles an instruction in moves.)
+__device__ __forceinline__ bool tc_elect() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
 // Arrives on `bar` once every product issued so far by this thread has ended.
 __device__ __forceinline__ void tc_commit(uint64_t* bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
