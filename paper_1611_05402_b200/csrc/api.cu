@@ -781,7 +781,7 @@ int zipml_project(zipml_ctx* ctx, const zipml_dataset* weights, const zipml_adap
     p.tokens = tokens; p.features = (int)weights->n; p.depth = (int)weights->m; p.bits = container_bits(weights->bits);
     p.lo = weights->feat_lo; p.step = weights->feat_step; p.center = code_center(weights->bits);
     p.ids = s.ids; p.sum = s.sum; p.hidden_scale = s.hidden_scale; p.hidden = s.hidden;
-    p.up = adapters ? adapters->b : nullptr; p.rank = rank;
+    p.up = adapters ? adapters->b : nullptr; p.rank = rank; p.requests = s.requests;
     p.out = Y; p.ldo = ldy; p.out_bf16 = dtype == ZIPML_BF16;
     p.early = capturing(ctx) ? 0 : copy ? 3 : 1;
     p.status = ctx->d_status;
@@ -835,7 +835,7 @@ int zipml_project_backward(zipml_ctx* ctx, const zipml_dataset* weights, const z
             p.tokens = tokens; p.features = (int)weights->m; p.depth = (int)weights->n; p.bits = container_bits(weights->bits);
             p.center = s.center;
             p.ids = s.ids; p.sum = s.sum; p.row_scale = s.row_scale; p.hidden_scale = s.hidden_scale; p.hidden = v;
-            p.up = adapters ? adapters->a : nullptr; p.rank = rank;
+            p.up = adapters ? adapters->a : nullptr; p.rank = rank; p.requests = s.requests;
             p.out = dX; p.ldo = lddx; p.out_bf16 = dtype == ZIPML_BF16;
             p.early = capturing(ctx) ? 0 : 3;
             p.status = ctx->d_status;

@@ -30,7 +30,8 @@ constexpr int kProjDepth = 64;                // depth of a stage: 128 bytes of 
 constexpr int kGroups = 3;                    // groups of unpacking warps, each with every third stage
 constexpr int kGroupWarps = 4;
 constexpr int kGroupThreads = 32 * kGroupWarps;
-constexpr int kProjThreads = 32 * (4 + kGroups * kGroupWarps);
+constexpr int kFirstPublisher = 4 + kGroups * kGroupWarps;     // a warp for each group
+constexpr int kProjThreads = 32 * (kFirstPublisher + kGroups);
 constexpr int kMostSlots = 12;
 constexpr int kRankChunk = 32;                // ranks of an adapter stage: high parts in the first half of the depth, low ones in the second
 constexpr uint32_t kLeftBytes = kProjRows * kProjDepth * 2;
@@ -41,12 +42,13 @@ constexpr uint32_t kLeftBytes = kProjRows * kProjDepth * 2;
 // cycles), in the left ring's order.  The groups' rings have a multiple of kGroups slots, so that a slot is always the same group's: a
 // barrier tells a phase from the one before it only, and a group that came to a slot whose last phase belonged to another could be a phase
 // early.
-template <int NT>
+template <int NT, bool PAIR>
 struct ProjShape {
     static constexpr int kLeft = 2 * kGroups;
-    static constexpr int kRight = NT == 256 ? 3 : NT == 128 ? 4 : 6;
-    static constexpr uint32_t kRightBytes = NT * kProjDepth * 2;
-    static constexpr uint32_t kCodeRing = (NT == 256 ? 3 : NT == 128 ? 6 : NT == 64 ? 9 : 12) * kProjRows * kProjDepth;     // bytes for packed codes
+    static constexpr int kRight = PAIR || NT == 128 ? 4 : 6;
+    static constexpr int kRightRows = PAIR ? NT / 2 : NT;               // tokens of the operand that lie in this CTA
+    static constexpr uint32_t kRightBytes = kRightRows * kProjDepth * 2;
+    static constexpr uint32_t kCodeRing = (NT >= 128 ? 6 : NT == 64 ? 9 : 12) * kProjRows * kProjDepth;     // bytes for packed codes
     static_assert(kRight >= kGroups && kRight <= kLeft && kLeft % kGroups == 0 && kMostSlots % kGroups == 0, "slots by group");
     static constexpr uint32_t kRing = kLeft * kLeftBytes + kRight * kRightBytes + kCodeRing;
     static constexpr uint32_t kColumns = NT == 16 ? 32 : 2 * NT;        // tensor memory: codes' sums, then adapters'
@@ -60,7 +62,7 @@ struct ProjToken {                            // what the epilogue needs of a to
 template <int NT>
 struct ProjShared {
     ProjToken token[NT];
-    uint64_t codes_full[kMostSlots], codes_empty[kMostSlots], full[2 * kGroups], empty[2 * kGroups];
+    uint64_t codes_full[kMostSlots], codes_empty[kMostSlots], written[2 * kGroups], full[2 * kGroups], empty[2 * kGroups];
     uint64_t up_full[kGroups], up_empty[kGroups], codes_done, done, plan;
     uint32_t tmem;
     int gave_up;
@@ -177,10 +179,10 @@ __device__ __forceinline__ uint32_t finite_pair(uint32_t w, uint32_t exponent, b
     return w;
 }
 
-template <int NT, bool BACK, bool BF16>
+template <int NT, bool BACK, bool BF16, bool PAIR>
 __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a, const __grid_constant__ CUtensorMap tokens_map,
                                                                   const __grid_constant__ CUtensorMap codes_map) {
-    using Shape = ProjShape<NT>;
+    using Shape = ProjShape<NT, PAIR>;
     constexpr int L = Shape::kLeft, R = Shape::kRight;
     extern __shared__ uint8_t raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -189,11 +191,14 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
     uint8_t* const right = ring + L * kLeftBytes;
     uint8_t* const packed = right + R * Shape::kRightBytes;
     cg::cluster_group cluster = cg::this_cluster();
-    const int crank = (int)cluster.block_rank(), cranks = (int)cluster.num_blocks();
+    // CTAs that divide the depth; a pair's two divide the features instead
+    const int side = PAIR ? (int)cluster.block_rank() : 0;
+    const int crank = PAIR ? 0 : (int)cluster.block_rank(), cranks = PAIR ? 1 : (int)cluster.num_blocks();
+    constexpr int kTileRows = PAIR ? 2 * kProjRows : kProjRows;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int feature_tiles = (a.features + kProjRows - 1) / kProjRows;
-    const int tile = blockIdx.x / cranks;
-    const int f0 = (tile % feature_tiles) * kProjRows;
+    const int feature_tiles = (a.features + kTileRows - 1) / kTileRows;
+    const int tile = PAIR ? blockIdx.x / 2 : blockIdx.x / cranks;
+    const int f0 = (tile % feature_tiles) * kTileRows + side * kProjRows;
     const int64_t t0 = (int64_t)(tile / feature_tiles) * NT;
     const int all_steps = (a.depth + kProjDepth - 1) / kProjDepth, per = (all_steps + cranks - 1) / cranks;
     const int step0 = min(crank * per, all_steps), steps = min(per, all_steps - step0);
@@ -208,11 +213,12 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             mbar_init(&sh.codes_empty[i], kGroupWarps);
         }
         for (int i = 0; i < L; ++i) {
-            mbar_init(&sh.full[i], 1 + kGroupWarps);                       // the tokens' copy and the unpacking warps
+            mbar_init(&sh.written[i], kGroupWarps);
+            mbar_init(&sh.full[i], 1 + (PAIR ? 2 : 1));                    // the tokens' copies and the publishing warps
             mbar_init(&sh.empty[i], 1);
         }
         for (int i = 0; i < kGroups; ++i) {
-            mbar_init(&sh.up_full[i], kGroupWarps);
+            mbar_init(&sh.up_full[i], (PAIR ? 2 : 1) * kGroupWarps);
             mbar_init(&sh.up_empty[i], 1);
         }
         mbar_init(&sh.codes_done, 1);
@@ -222,10 +228,11 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
         mbar_fence_init();
     }
     if (warp == 3) {
-        tc_alloc(&sh.tmem, Shape::kColumns);
+        tc_alloc<PAIR>(&sh.tmem, Shape::kColumns);
         tc_fence_before();
     }
     __syncthreads();
+    if constexpr (PAIR) cluster.sync();                               // (the other CTA's barriers and its tensor memory are there too)
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
     const int chunks = a.up ? (a.rank + kRankChunk - 1) / kRankChunk : 0;
@@ -242,11 +249,19 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                     if (!tc_wait(&sh.empty[ahead.slot], ahead.turn, gave_up, a.status, 93)) break;
                     ahead.next(1, L);
                 }
-                mbar_arrive_expect_tx(&sh.full[stage.slot], Shape::kRightBytes);
-                tc_copy_2d(smem_u32(right + at.slot * Shape::kRightBytes), &tokens_map, (step0 + s) * kProjDepth, (int)t0, &sh.full[stage.slot]);
+                const uint32_t dst = smem_u32(right + at.slot * Shape::kRightBytes);
+                if constexpr (PAIR) {
+                    // (both halves count on the first CTA's barrier; the other's bytes may come before they are expected)
+                    if (side == 0) mbar_arrive_expect_tx(&sh.full[stage.slot], 2 * Shape::kRightBytes);
+                    tc_copy_2d_pair(dst, &tokens_map, (step0 + s) * kProjDepth, (int)t0 + side * Shape::kRightRows, tc_peer(&sh.full[stage.slot], 0));
+                } else {
+                    mbar_arrive_expect_tx(&sh.full[stage.slot], Shape::kRightBytes);
+                    tc_copy_2d(dst, &tokens_map, (step0 + s) * kProjDepth, (int)t0, &sh.full[stage.slot]);
+                }
             }
             if (s < steps)                                                 // (its stages' barriers want the unpacking warps too: they are waited for a while)
-                for (int i = max(0, s - R); i < s; ++i) tc_drain(&sh.full[i % L], (i / L) & 1);
+                for (int i = max(0, s - R); i < s; ++i)
+                    if (side == 0) tc_drain(&sh.full[i % L], (i / L) & 1);
         }
     } else if (warp == 2) {
         // the packed codes
@@ -306,10 +321,11 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             if (found++ % cranks == crank) {
                 if (lane == 0) {
                     // (the first one takes every column, so that the others' sums start from zero)
-                    const int lo = entries == 0 ? 0 : first & ~15;
+                    // (and so does every one of a pair's, which holds the operand's tokens in two places)
+                    const int lo = entries == 0 || PAIR ? 0 : first & ~15;
                     sh.entry_id[entries] = id;
                     sh.entry_lo[entries] = lo;
-                    sh.entry_n[entries] = entries == 0 ? NT : (last + 16 - lo) & ~15;
+                    sh.entry_n[entries] = entries == 0 || PAIR ? NT : (last + 16 - lo) & ~15;
                 }
                 ++entries;
             }
@@ -318,10 +334,11 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
         __syncwarp();
         mbar_arrive(&sh.plan);
     } else if (warp == 1) {
-        // the products: the warp waits as a whole, one lane issues
+        // the products: the warp waits as a whole, one lane issues; of a pair, the first CTA's
+        if (side == 0) {
         bool ok = true;
         RingAt la, ra;
-        const uint32_t kind = tc_kind(BF16, !BACK, NT);
+        const uint32_t kind = tc_kind(BF16, !BACK, kTileRows, NT);
         // (operands by their first slot: an address in steps of 16 bytes is the description's lowest field)
         const uint64_t left_at = BACK ? tc_operand(smem_u32(left), 16, 1024) : tc_operand(smem_u32(left), kLeftBytes / 2, 1024);
         const uint64_t right_at = tc_operand(smem_u32(right), 16, 1024);
@@ -332,12 +349,12 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             const uint64_t lp = left_at + (uint32_t)la.slot * (kLeftBytes / 16), rp = right_at + (uint32_t)ra.slot * (Shape::kRightBytes / 16);
             if (tc_elect()) {
 #pragma unroll
-                for (int k = 0; k < kProjDepth / 16; ++k) tc_mma(tmem, lp + k * (BACK ? 2 : 128), rp + k * 2, kind, s > 0 || k > 0);
-                tc_commit(&sh.empty[la.slot]);
+                for (int k = 0; k < kProjDepth / 16; ++k) tc_mma<PAIR>(tmem, lp + k * (BACK ? 2 : 128), rp + k * 2, kind, s > 0 || k > 0);
+                tc_commit<PAIR>(&sh.empty[la.slot]);
             }
             __syncwarp();
         }
-        if (tc_elect()) tc_commit(&sh.codes_done);
+        if (tc_elect()) tc_commit<PAIR>(&sh.codes_done);
         __syncwarp();
         if (ok && chunks > 0) ok = __all_sync(0xffffffffu, tc_wait(&sh.plan, 0, gave_up, a.status, 97));
         if (ok && chunks > 0) {
@@ -350,22 +367,37 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 tc_fence_after();
                 const int lo = sh.entry_lo[e];
                 const uint64_t lp = up_at + (uint32_t)slot * (kLeftBytes / 16), rp = right_at + (uint32_t)slot * (Shape::kRightBytes / 16) + (uint32_t)lo * 8;
-                const uint32_t up_kind = tc_kind(BACK ? a.out_bf16 != 0 : BF16, true, sh.entry_n[e]);
+                const uint32_t up_kind = tc_kind(BACK ? a.out_bf16 != 0 : BF16, true, kTileRows, sh.entry_n[e]);
                 const int ks = (min(kRankChunk, a.rank - c * kRankChunk) + 15) / 16;
                 if (tc_elect()) {
                     for (int part = 0; part < 2; ++part)
                         for (int k = 0; k < ks; ++k)
-                            tc_mma(tmem + Shape::kColumns / 2 + lo, lp + k * 128, rp + part * 4 + k * 2, up_kind, j > 0 || part > 0 || k > 0);
-                    tc_commit(&sh.up_empty[slot]);
+                            tc_mma<PAIR>(tmem + Shape::kColumns / 2 + lo, lp + k * 128, rp + part * 4 + k * 2, up_kind, j > 0 || part > 0 || k > 0);
+                    tc_commit<PAIR>(&sh.up_empty[slot]);
                 }
                 __syncwarp();
             }
         }
         if (tc_elect()) {
-            tc_commit(&sh.done);
+            tc_commit<PAIR>(&sh.done);
             if (!ok) tc_drain(&sh.done, 0);
         }
         __syncwarp();
+        }
+    } else if (warp >= kFirstPublisher) {
+        // A group's stores, made visible to the tensor cores by a warp that has nothing else to do: the fence waits for what is on its way to
+        // shared memory, 500 to 1,400 cycles beside running products, which the unpacking warps spent idle.
+        RingAt la;
+        la.next(warp - kFirstPublisher, L);
+        for (int s = warp - kFirstPublisher; s < steps; s += kGroups, la.next(kGroups, L)) {
+            if (!__all_sync(0xffffffffu, tc_wait(&sh.written[la.slot], la.turn, gave_up, a.status, 106))) break;
+            tc_publish();
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR && side != 0) tc_arrive_at(tc_peer(&sh.full[la.slot], 0));
+                else mbar_arrive(&sh.full[la.slot]);
+            }
+        }
     } else {
         const int group = (warp - 4) / kGroupWarps, gid = (threadIdx.x - 128) % kGroupThreads;
         int s = group;
@@ -386,9 +418,8 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             else if (cb == 4) ok = unpack_stage<BF16, 4, BACK>(src, dst, gid, free, wait);
             else ok = unpack_stage<BF16, 2, BACK>(src, dst, gid, free, wait);
             if (!ok) break;
-            tc_publish();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.full[la.slot]);
+            if (lane == 0) mbar_arrive(&sh.written[la.slot]);
         }
         if (ok) ok = __all_sync(0xffffffffu, tc_wait(&sh.plan, 0, gave_up, a.status, 101));
         if (ok && chunks > 0) {
@@ -412,8 +443,9 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                     w[i] = make_uint4(0, 0, 0, 0);
                     if (k < rows) w[i] = load8_16(up + ((int64_t)id * a.rank + c * kRankChunk + k) * a.features + f, min(max(a.features - f, 0), 8), wide);
                 }
-                const int lo = sh.entry_lo[e], n = sh.entry_n[e], per_row = padded >> 3, units = n * per_row;
-                constexpr int V = 4;                                       // units of 8 ranks of a token, on their way together
+                const int lo = PAIR ? side * Shape::kRightRows : sh.entry_lo[e], n = PAIR ? Shape::kRightRows : sh.entry_n[e];
+                const int per_row = padded >> 3, units = n * per_row;
+                constexpr int V = 2;                                       // units of 8 ranks of a token, on their way together
                 float v[V][8];
                 const auto load = [&](int from) {
 #pragma unroll
@@ -470,14 +502,17 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                                 low[k] = pack_pair<__half>(v[i][2 * k] - f.x, v[i][2 * k + 1] - f.y);
                             }
                         }
-                        uint8_t* p = tok + t * 128;
+                        uint8_t* p = tok + (PAIR ? t - lo : t) * 128;
                         *reinterpret_cast<uint4*>(p + ((chunk ^ (t & 7)) << 4)) = make_uint4(high[0], high[1], high[2], high[3]);
                         *reinterpret_cast<uint4*>(p + (((chunk + 4) ^ (t & 7)) << 4)) = make_uint4(low[0], low[1], low[2], low[3]);
                     }
                 }
                 tc_publish();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.up_full[group]);
+                if (lane == 0) {
+                    if (PAIR && side != 0) tc_arrive_at(tc_peer(&sh.up_full[group], 0));
+                    else mbar_arrive(&sh.up_full[group]);
+                }
             }
             if (bad) set_status(a.status, ZIPML_ERR_NONFINITE, 103);
         }
@@ -498,10 +533,14 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             float* join = reinterpret_cast<float*>(ring);
             uint16_t* stage = reinterpret_cast<uint16_t*>(ring) + group * 2 * 16 * kProjRows;
             const bool wide_out = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * 2)) & 15) == 0;
+            uint32_t v[16], w[16];
+            const uint32_t lanes_at = tmem + ((uint32_t)(quarter * 32) << 16);
+            const auto load = [&](int c) {
+                if (steps > 0) tc_load16(lanes_at + c * 16, v);
+                if (have_up) tc_load16(lanes_at + Shape::kColumns / 2 + c * 16, w);
+            };
+            if (group < NT / 16) load(group);
             for (int c = group; c < NT / 16; c += kGroups) {
-                uint32_t v[16], w[16];
-                if (steps > 0) tc_load16(tmem + ((uint32_t)(quarter * 32) << 16) + c * 16, v);
-                if (have_up) tc_load16(tmem + ((uint32_t)(quarter * 32) << 16) + Shape::kColumns / 2 + c * 16, w);
                 tc_load_wait();
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -512,6 +551,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                     if (cranks > 1) join[(c * 16 + i) * kProjRows + row] = y;
                     else stage[i * kProjRows + row] = a.out_bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(y)) : __half_as_ushort(__float2half_rn(y));
                 }
+                if (c + kGroups < NT / 16) load(c + kGroups);             // (on its way while these rows go out)
                 if (cranks == 1) {
                     asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(kGroupThreads) : "memory");
 #pragma unroll
@@ -536,9 +576,10 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
         }
     }
     __syncthreads();
+    if constexpr (PAIR) cluster.sync();                               // (neither's memory goes while the other may still be at it)
     if (warp == 3) {
         tc_fence_after();
-        tc_free(tmem, Shape::kColumns);
+        tc_free<PAIR>(tmem, Shape::kColumns);
     }
     if (cranks > 1) {
         cluster.sync();
@@ -584,13 +625,15 @@ static int encode_map(zipml_ctx* ctx, CUtensorMapDataType type, const void* base
     return r == CUDA_SUCCESS ? ZIPML_OK : ZIPML_ERR_CUDA;
 }
 
-template <int NT, bool BACK, bool BF16>
+template <int NT, bool BACK, bool BF16, bool PAIR = false>
 static int launch_project_as(zipml_ctx* ctx, const ProjectArgs& a, const CUtensorMap& tokens_map, const CUtensorMap& codes_map, int ranks) {
-    auto kernel = &project_kernel<NT, BACK, BF16>;
-    const size_t smem = 1024 + ProjShape<NT>::kRing + sizeof(ProjShared<NT>);
+    auto kernel = &project_kernel<NT, BACK, BF16, PAIR>;
+    const size_t smem = 1024 + ProjShape<NT, PAIR>::kRing + sizeof(ProjShared<NT>);
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return cuda_status(e);
-    const int64_t tiles = (a.tokens + NT - 1) / NT * ((a.features + kProjRows - 1) / kProjRows);
+    constexpr int kTileRows = PAIR ? 2 * kProjRows : kProjRows;
+    if (PAIR) ranks = 2;
+    const int64_t tiles = (a.tokens + NT - 1) / NT * ((a.features + kTileRows - 1) / kTileRows);
     if (tiles * ranks > 0x7fffffffLL) return ZIPML_ERR_WORKSPACE;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(tiles * ranks));
@@ -612,40 +655,44 @@ static int launch_project_as(zipml_ctx* ctx, const ProjectArgs& a, const CUtenso
 // Tokens of a tile and CTAs that divide the depth, by the cycles that a wave of tiles should take: a stage is bound by shared memory
 // (both operands are read by the tensor core and the left one written by the unpacking warps, 128 bytes a cycle: NT + 256), a tile also pays for
 // its start, its epilogue and, where the depth is divided, the exchange.
-static void project_shape(const zipml_ctx* ctx, const ProjectArgs& a, int* tokens, int* ranks) {
+// Pairs of CTAs halve what a stage of 256 tokens reads and keeps of them (NT / 2 + 256, the product's own 2 NT at least).
+static void project_shape(const zipml_ctx* ctx, const ProjectArgs& a, int* tokens, int* ranks, bool* pair) {
     const int64_t feature_tiles = (a.features + kProjRows - 1) / kProjRows, steps = (a.depth + kProjDepth - 1) / kProjDepth;
     double best = 0.0;
     for (const int nt : {16, 64, 128, 256})
         for (int r = 1; r <= (nt == 256 ? 1 : 8); r *= 2) {
             if (r > 1 && steps / r < 4) break;
+            if (nt == 256 && a.up && a.tokens < (int64_t)a.requests * 32) break;      // (a pair takes all of a tile's columns for each adapter)
             const int64_t ctas = (a.tokens + nt - 1) / nt * feature_tiles * r;
             const int64_t waves = (ctas + ctx->sm_count - 1) / ctx->sm_count;
-            const double cycles = (double)waves * ((double)((steps + r - 1) / r) * (nt + 256) + 3000 + nt * 16 + (r > 1 ? 1500 : 0));
+            const double cycles = (double)waves * ((double)((steps + r - 1) / r) * (nt == 256 ? 600 : nt + 256) + 3000 + nt * 16 + (r > 1 ? 1500 : 0));
             if (best == 0.0 || cycles < best) { best = cycles; *tokens = nt; *ranks = r; }
         }
+    *pair = *tokens == 256;
 }
 
 template <bool BACK, bool BF16>
-static int launch_project_typed(zipml_ctx* ctx, const ProjectArgs& a, const CUtensorMap& tm, const CUtensorMap& cm, int nt, int ranks) {
+static int launch_project_typed(zipml_ctx* ctx, const ProjectArgs& a, const CUtensorMap& tm, const CUtensorMap& cm, int nt, int ranks, bool pair) {
+    if (pair) return launch_project_as<256, BACK, BF16, true>(ctx, a, tm, cm, ranks);
     if (nt == 16) return launch_project_as<16, BACK, BF16>(ctx, a, tm, cm, ranks);
     if (nt == 64) return launch_project_as<64, BACK, BF16>(ctx, a, tm, cm, ranks);
-    if (nt == 128) return launch_project_as<128, BACK, BF16>(ctx, a, tm, cm, ranks);
-    return launch_project_as<256, BACK, BF16>(ctx, a, tm, cm, ranks);
+    return launch_project_as<128, BACK, BF16>(ctx, a, tm, cm, ranks);
 }
 
 int launch_project(zipml_ctx* ctx, const ProjectArgs& a, const void* tokens_operand, int64_t ld_operand, bool operand_bf16, const zipml_dataset* w, bool backward) {
     int nt = 16, ranks = 1;
-    project_shape(ctx, a, &nt, &ranks);
+    bool pair = false;
+    project_shape(ctx, a, &nt, &ranks, &pair);
     CUtensorMap tokens_map, codes_map;
     int rc = encode_map(ctx, operand_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, tokens_operand, a.depth, a.tokens, ld_operand * 2,
-                        kProjDepth, nt, CU_TENSOR_MAP_SWIZZLE_128B, &tokens_map);
+                        kProjDepth, pair ? nt / 2 : nt, CU_TENSOR_MAP_SWIZZLE_128B, &tokens_map);
     if (rc != ZIPML_OK) return rc;
     rc = encode_map(ctx, CU_TENSOR_MAP_DATA_TYPE_UINT8, w->plane1, w->row_bytes, w->m, w->row_bytes, (backward ? kProjDepth : kProjRows) * a.bits / 8,
                     backward ? kProjRows : kProjDepth, CU_TENSOR_MAP_SWIZZLE_NONE, &codes_map);
     if (rc != ZIPML_OK) return rc;
-    if (backward) return launch_project_typed<true, false>(ctx, a, tokens_map, codes_map, nt, ranks);
-    return operand_bf16 ? launch_project_typed<false, true>(ctx, a, tokens_map, codes_map, nt, ranks)
-                        : launch_project_typed<false, false>(ctx, a, tokens_map, codes_map, nt, ranks);
+    if (backward) return launch_project_typed<true, false>(ctx, a, tokens_map, codes_map, nt, ranks, pair);
+    return operand_bf16 ? launch_project_typed<false, true>(ctx, a, tokens_map, codes_map, nt, ranks, pair)
+                        : launch_project_typed<false, false>(ctx, a, tokens_map, codes_map, nt, ranks, pair);
 }
 
 }  // namespace zipml

@@ -117,7 +117,7 @@ struct ProjectArgs {
     const int* ids;
     const float *sum, *row_scale, *hidden_scale, *hidden;   // row_scale may be null
     const void* up;              // adapters x rank x features, or null
-    int rank;
+    int rank, requests;
     void* out;
     int64_t ldo;
     int out_bf16;

@@ -319,6 +319,9 @@ SHAPES = [
     (130, 1024, 2049, 4, 40, 6, [1, 128, 1]),
     (300, 256, 1200, 7, 16, 7, [100, 57, 3, 140]),
     (700, 520, 2600, 8, 8, 3, [256, 256, 188]),
+    (1500, 700, 3001, 4, 24, 3, [700, 1, 500, 299]),
+    (1500, 3100, 650, 8, 40, 4, [100, 900, 499, 1]),
+    (1291, 2304, 2304, 2, 16, 9, [128] * 10 + [11]),
 ]
 
 
