@@ -604,8 +604,8 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
     }
 }
 
-static int encode_map(zipml_ctx* ctx, CUtensorMapDataType type, const void* base, int64_t inner, int64_t rows, int64_t stride_bytes, int box_inner, int box_rows,
-                      CUtensorMapSwizzle swizzle, CUtensorMap* out) {
+int encode_map(zipml_ctx* ctx, CUtensorMapDataType type, const void* base, int64_t inner, int64_t rows, int64_t stride_bytes, int box_inner, int box_rows,
+               CUtensorMapSwizzle swizzle, CUtensorMap* out) {
     typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
     if (!ctx->tmap_encode) {

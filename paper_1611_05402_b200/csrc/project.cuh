@@ -138,10 +138,15 @@ struct GradArgs {
     const void* dy;              // tokens x lddy
     int64_t lddy;
     int outputs, bf16;
+    int dy_copied;               // dy's rows are aligned for tensor copies
     float *grad_down, *grad_up;  // either may be null
     int down_blocks, up_blocks;
     DeviceStatus* status;
 };
+
+// Tensor map of a matrix of `rows` rows (project.cu).
+int encode_map(zipml_ctx* ctx, CUtensorMapDataType type, const void* base, int64_t inner, int64_t rows, int64_t stride_bytes, int box_inner, int box_rows,
+               CUtensorMapSwizzle swizzle, CUtensorMap* out);
 
 int launch_shrink(zipml_ctx* ctx, const ShrinkArgs& a, int dtype, bool backward);
 int launch_project(zipml_ctx* ctx, const ProjectArgs& a, const void* tokens_operand, int64_t ld_operand, bool operand_bf16, const zipml_dataset* w,

@@ -3,140 +3,246 @@
 #include <cooperative_groups.h>
 
 #include "project.cuh"
+#include "tensor_core.cuh"
 
 namespace zipml {
 
 namespace cg = cooperative_groups;
 
 // ---------------------------------------------------------------------------------------------
-// A cluster takes one adapter and one block of columns (128 codes or 64 values of dy: 128 bytes of each row), its CTAs' warps the
-// adapter's tokens in turns of 8.  m16n8k8 products in tf32, ranks x columns x tokens: codes (code - 128) and 16-bit values are exact in
-// its 11 bits, v step and hidden are split into two such parts, so a product keeps 22 bits.  A lane reads 16 consecutive bytes of
-// the rows of two tokens; byte f of eight lanes is the f-th block of columns.  The lower ends' share, v . (lo + 128 step), is the same for a
-// group's columns and is summed once per group.  Warps' and CTAs' sums are added in a fixed order.
+// A cluster takes one adapter and one block of columns (128 codes or 64 values of dy: 128 bytes of each row), its CTAs' warps the adapter's
+// tokens in chunks of 32 in turn.  Every warp has slots of 4 KB of its own and keeps them on their way (tensor copies with the 128-byte
+// swizzle; rows of dy that these cannot take are read straight from global memory): nothing is handed from warp to warp before the
+// end.  m16n8k8 products in tf32, ranks x columns x tokens: codes (code - 128) and 16-bit values are exact in its 11 bits, v step and
+// hidden are split into two such parts, so a product keeps 22 bits.  A lane reads 16 consecutive bytes of the rows of two tokens; byte f of
+// eight lanes is the f-th block of columns.  The two tokens of a lane are neighbours, which with the swizzle is free of bank
+// conflicts.  The lower ends' share, v . (lo + 128 step), is the same for a group's columns and is summed once per group.  Warps' and CTAs'
+// sums are added in a fixed order.
 // ---------------------------------------------------------------------------------------------
 constexpr int kGradWarps = 8;
+constexpr int kGradThreads = 32 * kGradWarps;
+constexpr int kGradChunk = 32;                          // tokens
+constexpr uint32_t kGradSlotBytes = kGradChunk * 128;
+constexpr int kGradBatch = kGradThreads;                // requests that are looked at together
+// Slots of a warp: two CTAs of an SM for up to 16 ranks, one (by its registers) for 32.
+__host__ __device__ constexpr int grad_slots(int mt) { return mt == 1 ? 3 : 6; }
+constexpr int kGradMostSlots = 6;
+
+struct GradShared {
+    uint64_t full[kGradWarps][kGradMostSlots];
+    int gave_up;
+    int found[kGradWarps];
+    int segments;
+    int begin[kGradBatch], end[kGradBatch];             // this adapter's token ranges among the batch's requests
+};
 
 __device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&x)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(b0), "r"(b1));
 }
+// byte i of a word, less 128 (see byte_to_float)
+__device__ __forceinline__ float centred_code(uint32_t bytes, int i) { return __uint_as_float(__byte_perm(bytes, 0x4B000000u, 0x7650 + i)) - 8388736.0f; }
 // x = high + low, both within tf32's 11 bits up to 2^-22 of x
 __device__ __forceinline__ void split_tf32(float x, uint32_t& high, uint32_t& low) {
     high = __float_as_uint(x) & 0xffffe000u;
     low = __float_as_uint(x - __uint_as_float(high));
 }
 
-// MT: blocks of 16 ranks.  A pass takes at most kPassBlocks of them (registers), so higher ranks read the rows more than once.
-template <bool CODES, int MT>
-__device__ __forceinline__ void grad_pass(const GradArgs& a, int adapter, int block, int r0, float* sums, cg::cluster_group& cluster) {
-    constexpr int NF = CODES ? 16 : 8;                     // columns of a lane's 16 bytes
-    constexpr int GROUPS = CODES ? 4 : 1;                  // grids that 128 codes can lie in
+// The left factors and grids of 8 tokens, as a lane needs them: ranks g and g + 8 of each block, tokens 2 q and 2 q + 1.
+template <int GROUPS, int MT>
+struct GradLeft {
+    float v[MT][4];
+    float2 grid[GROUPS][2];
+};
+
+// GROUPS: grids that a block of columns lies in (1, or 4 where groups may be narrower than 128), 0 for the values of dy.  MT: blocks of 16
+// ranks, 1 or 2 (registers); higher ranks read the rows once for each 32.
+template <int GROUPS, int MT>
+__device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* map, int adapter, int block, int r0, uint8_t* ring, GradShared& sh,
+                                          cg::cluster_group& cluster) {
+    constexpr bool CODES = GROUPS > 0;
+    constexpr int GR = CODES ? GROUPS : 1, NF = CODES ? 16 : 8;            // NF: columns of a lane's 16 bytes
+    constexpr int SLOTS = grad_slots(MT);
+    using Left = GradLeft<GR, MT>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int ranks = (int)cluster.num_blocks(), crank = (int)cluster.block_rank();
     const int columns = CODES ? a.inputs : a.outputs;
     const int col0 = block * NF * 8, lane_col = col0 + g * NF;
+    const bool copied = CODES || a.dy_copied;
     const float* left = CODES ? a.v : a.hidden;
+    const int per = GROUPS == 4 ? 128 / a.group : 1;       // grids in the block
+    volatile int* gave_up = &sh.gave_up;
+    uint8_t* slots = ring + warp * SLOTS * kGradSlotBytes;
     float acc[MT][NF][4] = {};
-    float base[MT][GROUPS][2] = {};
-    int turn = crank * kGradWarps + warp;                  // chunks of 8 tokens until this warp's next one
-    for (int req = 0; req < a.requests; ++req) {
-        if (a.which[req] != adapter) continue;
-        const int64_t s = max((int64_t)a.starts[req], (int64_t)0), e = min((int64_t)a.starts[req + 1], a.tokens);
-        if (e <= s) continue;
-        const int64_t chunks = (e - s + 7) >> 3;
-        int64_t c = turn;
-        for (; c < chunks; c += ranks * kGradWarps) {
-            const int64_t t0 = s + c * 8 + q, t1 = t0 + 4;
-            const bool in0 = t0 < e, in1 = t1 < e;
-            uint4 w0 = make_uint4(0, 0, 0, 0), w1 = w0;
-            if constexpr (CODES) {
-                if (lane_col < a.code_stride) {
-                    if (in0) w0 = *reinterpret_cast<const uint4*>(a.codes + t0 * a.code_stride + lane_col);
-                    if (in1) w1 = *reinterpret_cast<const uint4*>(a.codes + t1 * a.code_stride + lane_col);
-                }
-            } else {
-                const uint16_t* dy = reinterpret_cast<const uint16_t*>(a.dy);
-                const bool wide = ((reinterpret_cast<uintptr_t>(dy) | (uintptr_t)(a.lddy * 2)) & 15) == 0;
-                const int count = min(max(columns - lane_col, 0), 8);
-                if (in0) w0 = load8_16(dy + t0 * a.lddy + lane_col, count, wide);
-                if (in1) w1 = load8_16(dy + t1 * a.lddy + lane_col, count, wide);
+    float base[MT][GR][2] = {};
+    const int others = ranks * kGradWarps, me = crank * kGradWarps + warp; // (a power of two of warps take the chunks in turn)
+    int turn = 0;                                          // chunks of the batches so far, of all warps
+    uint32_t taken = 0, issued = 0;                        // of this one
+    for (int first = 0; first < a.requests; first += kGradBatch) {
+        // the batch's requests of this adapter, in order
+        __syncthreads();
+        {
+            const int req = first + (int)threadIdx.x;
+            int s = 0, e = 0;
+            if (req < a.requests && a.which[req] == adapter) {
+                s = max(a.starts[req], 0);
+                e = (int)min((int64_t)a.starts[req + 1], a.tokens);
             }
-            // the left factor of (rank g or g + 8 of each block, token t0 or t1)
-            float v[MT][4];
+            const uint32_t has = __ballot_sync(0xffffffffu, e > s);
+            if (lane == 0) sh.found[warp] = __popc(has);
+            __syncthreads();
+            int at = __popc(has & ((1u << lane) - 1u));
+            for (int w = 0; w < warp; ++w) at += sh.found[w];
+            if (e > s) { sh.begin[at] = s; sh.end[at] = e; }
+            if (threadIdx.x == kGradThreads - 1) sh.segments = at + (e > s);
+        }
+        __syncthreads();
+        const int segments = sh.segments;
+        struct Cursor { int i, c, turn; };                 // chunk c of range i, the turn-th of all warps' chunks
+        const auto settle = [&](Cursor& at) {              // on to the next chunk that is this warp's
+            while (at.i < segments) {
+                const int chunks = (sh.end[at.i] - sh.begin[at.i] + kGradChunk - 1) / kGradChunk;
+                const int skip = (me - at.turn) & (others - 1);
+                if (at.c + skip < chunks) { at.c += skip; at.turn += skip; return; }
+                at.turn += chunks - at.c;
+                ++at.i;
+                at.c = 0;
+            }
+        };
+        const auto step = [&](Cursor& at) { ++at.c; ++at.turn; settle(at); };
+        Cursor ahead{0, 0, turn};
+        const auto issue = [&] {                           // (into the slot that was read longest ago, by this warp)
+            if (ahead.i >= segments) return;
+            const uint32_t slot = issued % SLOTS;
+            if (lane == 0) {
+                mbar_arrive_expect_tx(&sh.full[warp][slot], kGradSlotBytes);
+                tc_copy_2d(smem_u32(slots + slot * kGradSlotBytes), map, col0, sh.begin[ahead.i] + ahead.c * kGradChunk, &sh.full[warp][slot]);
+            }
+            ++issued;
+            step(ahead);
+        };
+        if (copied) {
+            settle(ahead);
+            for (int k = 0; k < SLOTS; ++k) issue();
+        }
+        const auto load_left = [&](Left& l, int t, int e) {
+            const bool in0 = t < e, in1 = t + 1 < e;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 const int ra = r0 + m * 16 + g, rb = ra + 8;
-                v[m][0] = in0 && ra < a.rank ? left[t0 * a.rank + ra] : 0.0f;
-                v[m][1] = in0 && rb < a.rank ? left[t0 * a.rank + rb] : 0.0f;
-                v[m][2] = in1 && ra < a.rank ? left[t1 * a.rank + ra] : 0.0f;
-                v[m][3] = in1 && rb < a.rank ? left[t1 * a.rank + rb] : 0.0f;
+                const float* p = left + (int64_t)t * a.rank;
+                l.v[m][0] = in0 && ra < a.rank ? p[ra] : 0.0f;
+                l.v[m][1] = in0 && rb < a.rank ? p[rb] : 0.0f;
+                l.v[m][2] = in1 && ra < a.rank ? p[a.rank + ra] : 0.0f;
+                l.v[m][3] = in1 && rb < a.rank ? p[a.rank + rb] : 0.0f;
             }
-            const uint32_t u0[4] = {w0.x, w0.y, w0.z, w0.w}, u1[4] = {w1.x, w1.y, w1.z, w1.w};
             if constexpr (CODES) {
-                // Where the block holds several groups, each takes a product of its own, with v times its step on the left and the other
-                // groups' columns zero on the right.
-                const int per = max(1, 128 / a.group);     // grids in the block: 1, 2 or 4
-                for (int k = 0; k < per; ++k) {
-                    const int grid = (col0 + k * a.group) / a.group;
-                    if (col0 + k * a.group >= columns) break;
-                    const float2 g0 = in0 ? a.grids[t0 * a.groups + grid] : make_float2(0.0f, 0.0f);
-                    const float2 g1 = in1 ? a.grids[t1 * a.groups + grid] : make_float2(0.0f, 0.0f);
-                    const float m0 = fmaf(128.0f, g0.y, g0.x), m1 = fmaf(128.0f, g1.y, g1.x);
-                    const bool own = per == 1 || (g * NF) / a.group == k;
-                    uint32_t hi[MT][4], lo[MT][4];
+                const float2 none = make_float2(0.0f, 0.0f);
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        split_tf32(v[m][0] * g0.y, hi[m][0], lo[m][0]);
-                        split_tf32(v[m][1] * g0.y, hi[m][1], lo[m][1]);
-                        split_tf32(v[m][2] * g1.y, hi[m][2], lo[m][2]);
-                        split_tf32(v[m][3] * g1.y, hi[m][3], lo[m][3]);
+                for (int k = 0; k < GR; ++k) {
+                    const bool there = k < per && col0 + k * a.group < columns;
+                    const int64_t at = (int64_t)t * a.groups + (col0 + k * a.group) / a.group;
+                    l.grid[k][0] = there && in0 ? a.grids[at] : none;
+                    l.grid[k][1] = there && in1 ? a.grids[at + a.groups] : none;
+                }
+            }
+        };
+        Left next;
+        Cursor at{0, 0, turn};
+        settle(at);
+        if (at.i < segments) load_left(next, sh.begin[at.i] + at.c * kGradChunk + 2 * q, sh.end[at.i]);
+        while (at.i < segments) {
+            const int t0 = sh.begin[at.i] + at.c * kGradChunk, e = sh.end[at.i];
+            step(at);
+            const uint32_t slot = taken % SLOTS;
+            if (copied && !__all_sync(0xffffffffu, tc_wait(&sh.full[warp][slot], (taken / SLOTS) & 1, gave_up, a.status, 108))) break;
+#pragma unroll 1
+            for (int tt = 0; tt < kGradChunk && t0 + tt < e; tt += 8) {
+                const Left l = next;
+                const int t = t0 + tt + 2 * q;
+                const bool in0 = t < e, in1 = t + 1 < e;
+                if (tt + 8 < kGradChunk && t0 + tt + 8 < e) load_left(next, t + 8, e);
+                else if (at.i < segments) load_left(next, sh.begin[at.i] + at.c * kGradChunk + 2 * q, sh.end[at.i]);
+                uint4 w0 = make_uint4(0, 0, 0, 0), w1 = w0;
+                if (copied) {
+                    const uint8_t* p = slots + slot * kGradSlotBytes + (tt + 2 * q) * 128;
+                    w0 = *reinterpret_cast<const uint4*>(p + ((g ^ (2 * q)) << 4));
+                    w1 = *reinterpret_cast<const uint4*>(p + 128 + ((g ^ (2 * q + 1)) << 4));
+                } else {
+                    const uint16_t* dy = reinterpret_cast<const uint16_t*>(a.dy) + (int64_t)t * a.lddy + lane_col;
+                    const int count = min(max(columns - lane_col, 0), 8);
+                    if (in0) w0 = load8_16(dy, count, false);
+                    if (in1) w1 = load8_16(dy + a.lddy, count, false);
+                }
+                if (!CODES) {                              // (what lies behind the range belongs to others and need not be finite)
+                    if (!in0) w0 = make_uint4(0, 0, 0, 0);
+                    if (!in1) w1 = make_uint4(0, 0, 0, 0);
+                }
+                const uint32_t u0[4] = {w0.x, w0.y, w0.z, w0.w}, u1[4] = {w1.x, w1.y, w1.z, w1.w};
+                if constexpr (CODES) {
+                    // Where the block holds several groups, each takes a product of its own, with v times its step on the left and the other
+                    // groups' columns zero on the right.
 #pragma unroll
-                        for (int kk = 0; kk < GROUPS; ++kk)
-                            if (kk == k) {
-                                base[m][kk][0] += fmaf(v[m][0], m0, v[m][2] * m1);
-                                base[m][kk][1] += fmaf(v[m][1], m0, v[m][3] * m1);
-                            }
-                    }
-#pragma unroll
-                    for (int f = 0; f < NF; ++f) {
-                        const float b0 = own ? byte_to_float(u0[f >> 2], f & 3) - 128.0f : 0.0f;
-                        const float b1 = own ? byte_to_float(u1[f >> 2], f & 3) - 128.0f : 0.0f;
+                    for (int k = 0; k < GR; ++k) {
+                        if (k >= per) break;
+                        const float2 g0 = l.grid[k][0], g1 = l.grid[k][1];
+                        const float m0 = fmaf(128.0f, g0.y, g0.x), m1 = fmaf(128.0f, g1.y, g1.x);
+                        const bool own = GR == 1 || (g * NF) / a.group == k;
+                        uint32_t hi[MT][4], lo[MT][4];
 #pragma unroll
                         for (int m = 0; m < MT; ++m) {
-                            mma_tf32(acc[m][f], hi[m], __float_as_uint(b0), __float_as_uint(b1));
-                            mma_tf32(acc[m][f], lo[m], __float_as_uint(b0), __float_as_uint(b1));
+                            split_tf32(l.v[m][0] * g0.y, hi[m][0], lo[m][0]);
+                            split_tf32(l.v[m][1] * g0.y, hi[m][1], lo[m][1]);
+                            split_tf32(l.v[m][2] * g1.y, hi[m][2], lo[m][2]);
+                            split_tf32(l.v[m][3] * g1.y, hi[m][3], lo[m][3]);
+                            base[m][k][0] += fmaf(l.v[m][0], m0, l.v[m][2] * m1);
+                            base[m][k][1] += fmaf(l.v[m][1], m0, l.v[m][3] * m1);
+                        }
+#pragma unroll
+                        for (int f = 0; f < NF; ++f) {
+                            const float b0 = own ? centred_code(u0[f >> 2], f & 3) : 0.0f, b1 = own ? centred_code(u1[f >> 2], f & 3) : 0.0f;
+#pragma unroll
+                            for (int m = 0; m < MT; ++m) {
+                                mma_tf32(acc[m][f], hi[m], __float_as_uint(b0), __float_as_uint(b1));
+                                mma_tf32(acc[m][f], lo[m], __float_as_uint(b0), __float_as_uint(b1));
+                            }
+                        }
+                    }
+                } else {
+                    uint32_t hi[MT][4], lo[MT][4];
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) split_tf32(l.v[m][k], hi[m][k], lo[m][k]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float2 b0 = a.bf16 ? unpack_pair<__nv_bfloat16>(u0[k]) : unpack_pair<__half>(u0[k]);
+                        const float2 b1 = a.bf16 ? unpack_pair<__nv_bfloat16>(u1[k]) : unpack_pair<__half>(u1[k]);
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) {
+                            mma_tf32(acc[m][2 * k], hi[m], __float_as_uint(b0.x), __float_as_uint(b1.x));
+                            mma_tf32(acc[m][2 * k], lo[m], __float_as_uint(b0.x), __float_as_uint(b1.x));
+                            mma_tf32(acc[m][2 * k + 1], hi[m], __float_as_uint(b0.y), __float_as_uint(b1.y));
+                            mma_tf32(acc[m][2 * k + 1], lo[m], __float_as_uint(b0.y), __float_as_uint(b1.y));
                         }
                     }
                 }
-            } else {
-                uint32_t hi[MT][4], lo[MT][4];
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) split_tf32(v[m][i], hi[m][i], lo[m][i]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 b0 = a.bf16 ? unpack_pair<__nv_bfloat16>(u0[i]) : unpack_pair<__half>(u0[i]);
-                    const float2 b1 = a.bf16 ? unpack_pair<__nv_bfloat16>(u1[i]) : unpack_pair<__half>(u1[i]);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        mma_tf32(acc[m][2 * i], hi[m], __float_as_uint(b0.x), __float_as_uint(b1.x));
-                        mma_tf32(acc[m][2 * i], lo[m], __float_as_uint(b0.x), __float_as_uint(b1.x));
-                        mma_tf32(acc[m][2 * i + 1], hi[m], __float_as_uint(b0.y), __float_as_uint(b1.y));
-                        mma_tf32(acc[m][2 * i + 1], lo[m], __float_as_uint(b0.y), __float_as_uint(b1.y));
-                    }
-                }
+            }
+            if (copied) {
+                __syncwarp();
+                ++taken;
+                issue();
             }
         }
-        turn = (int)(c - chunks);                          // (the next request's chunks go on where this one's ended)
+        turn = at.turn;
     }
+    if (*gave_up && lane == 0)                             // (copies that nobody has waited for)
+        for (; taken < issued; ++taken) tc_drain(&sh.full[warp][taken % SLOTS], (taken / SLOTS) & 1);
     if constexpr (CODES) {
-        const int per = max(1, 128 / a.group);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
 #pragma unroll
-            for (int k = 0; k < GROUPS; ++k)
+            for (int k = 0; k < GR; ++k)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     float s = base[m][k][i];
@@ -147,62 +253,82 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, int adapter, int bl
             // column n of the product's blocks is lane n's 16 codes: columns 2 q and 2 q + 1 here
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const int k = per == 1 ? 0 : ((2 * q + half) * NF) / a.group;
+                const int mine = GR == 1 ? 0 : ((2 * q + half) * NF) / a.group;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const float s = k == 0 ? base[m][0][i] : k == 1 ? base[m][1][i] : k == 2 ? base[m][2][i] : base[m][3][i];
+                    float s = base[m][0][i];
+#pragma unroll
+                    for (int k = 1; k < GR; ++k)
+                        if (mine == k) s = base[m][k][i];
 #pragma unroll
                     for (int f = 0; f < NF; ++f) acc[m][f][2 * i + half] += s;
                 }
             }
         }
     }
-    // Sums over the warps, then over the CTAs: [rank of the pass][column], one warp after the other
+    // Sums over the warps, then over the CTAs, 16 ranks at a time: [warp][rank][column] in the ring's place, 16 bytes at a position that the
+    // eight lanes of a store share no bank in.
     constexpr int C = NF * 8;
-    for (int w = 0; w < kGradWarps; ++w) {
-        if (warp == w)
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int f = 0; f < NF; ++f)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float* p = sums + (m * 16 + g + 8 * (i >> 1)) * C + (2 * q + (i & 1)) * NF + f;
-                        *p = w == 0 ? acc[m][f][i] : *p + acc[m][f][i];
-                    }
-        __syncthreads();
-    }
-    cluster.sync();
     float* out = CODES ? a.grad_down : a.grad_up;
-    const int most = min(MT * 16, a.rank - r0);
-    for (int i = crank * blockDim.x + threadIdx.x; i < most * C; i += ranks * blockDim.x) {
-        const int r = i / C, col = col0 + i % C;
-        float s = 0.0f;
-        for (int c = 0; c < ranks; ++c) s += cluster.map_shared_rank(sums, c)[i];
-        if (col < columns) out[((int64_t)adapter * a.rank + r0 + r) * columns + col] = s;
+    float* sums = reinterpret_cast<float*>(ring);
+    const auto place = [](int r, int col) { return r * C + (((col >> 2) ^ ((col >> (CODES ? 5 : 4)) & 3) ^ ((r & 1) << 2)) << 2) + (col & 3); };
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        __syncthreads();                                   // (the ring has been read, the sums before have been taken)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int f = 0; f < NF; f += 4)
+                *reinterpret_cast<float4*>(sums + warp * 16 * C + place(g + 8 * (i >> 1), (2 * q + (i & 1)) * NF + f)) =
+                    make_float4(acc[m][f][i], acc[m][f + 1][i], acc[m][f + 2][i], acc[m][f + 3][i]);
+        __syncthreads();
+        for (int i = threadIdx.x; i < 16 * C; i += kGradThreads) {
+            float s = sums[i];
+#pragma unroll
+            for (int w = 1; w < kGradWarps; ++w) s += sums[w * 16 * C + i];
+            sums[i] = s;
+        }
+        cluster.sync();
+        const int most = min(16, a.rank - r0 - m * 16);
+        for (int i = crank * kGradThreads + threadIdx.x; i < most * C; i += ranks * kGradThreads) {
+            const int r = i / C, col = i % C;
+            float s = 0.0f;
+            for (int c = 0; c < ranks; ++c) s += cluster.map_shared_rank(sums, c)[place(r, col)];
+            if (col0 + col < columns) out[((int64_t)adapter * a.rank + r0 + m * 16 + r) * columns + col0 + col] = s;
+        }
+        cluster.sync();
     }
-    cluster.sync();
 }
 
 template <int MT>
-__global__ void __launch_bounds__(32 * kGradWarps) grad_kernel(GradArgs a) {
-    extern __shared__ float sums[];
+__global__ void __launch_bounds__(kGradThreads, MT == 1 ? 2 : 1) grad_kernel(GradArgs a, const __grid_constant__ CUtensorMap codes_map, const __grid_constant__ CUtensorMap dy_map) {
+    extern __shared__ uint8_t raw[];
+    uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    GradShared& sh = *reinterpret_cast<GradShared*>(ring + kGradWarps * grad_slots(MT) * kGradSlotBytes);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kGradWarps * kGradMostSlots; ++i) mbar_init(&sh.full[0][0] + i, 1);
+        sh.gave_up = 0;
+        mbar_fence_init();
+    }
     cg::cluster_group cluster = cg::this_cluster();
     const int block = blockIdx.x / cluster.num_blocks(), adapter = blockIdx.y, r0 = blockIdx.z * MT * 16;
-    if (block < a.down_blocks) grad_pass<true, MT>(a, adapter, block, r0, sums, cluster);
-    else grad_pass<false, MT>(a, adapter, block - a.down_blocks, r0, sums, cluster);
+    if (block >= a.down_blocks) grad_pass<0, MT>(a, &dy_map, adapter, block - a.down_blocks, r0, ring, sh, cluster);
+    else if (a.group >= 128) grad_pass<1, MT>(a, &codes_map, adapter, block, r0, ring, sh, cluster);
+    else grad_pass<4, MT>(a, &codes_map, adapter, block, r0, ring, sh, cluster);
 }
 
 template <int MT>
-static int launch_grad_as(zipml_ctx* ctx, const GradArgs& a) {
+static int launch_grad_as(zipml_ctx* ctx, const GradArgs& a, const CUtensorMap& codes_map, const CUtensorMap& dy_map) {
     const int blocks = a.down_blocks + a.up_blocks, passes = (a.rank + MT * 16 - 1) / (MT * 16);
-    const size_t smem = (size_t)MT * 16 * 128 * sizeof(float);
+    const size_t smem = 1024 + kGradWarps * grad_slots(MT) * kGradSlotBytes + sizeof(GradShared);
+    cudaError_t e = cudaFuncSetAttribute(&grad_kernel<MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return cuda_status(e);
     int ranks = 1;
-    while (ranks < 8 && (int64_t)blocks * a.adapters * passes * ranks < 2 * ctx->sm_count && (int64_t)ranks * kGradWarps * 8 < a.tokens) ranks *= 2;
+    while (ranks < 8 && (int64_t)blocks * a.adapters * passes * ranks < 2 * ctx->sm_count && (int64_t)ranks * kGradWarps * kGradChunk < a.tokens) ranks *= 2;
     if (a.adapters > 65535 || (int64_t)blocks * ranks > 0x7fffffffLL) return ZIPML_ERR_WORKSPACE;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(blocks * ranks), (unsigned)a.adapters, (unsigned)passes);
-    cfg.blockDim = dim3(32 * kGradWarps);
+    cfg.blockDim = dim3(kGradThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = ctx->stream;
     cudaLaunchAttribute attr[1];
@@ -210,7 +336,7 @@ static int launch_grad_as(zipml_ctx* ctx, const GradArgs& a) {
     attr[0].val.clusterDim.x = (unsigned)ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, &grad_kernel<MT>, a);
+    e = cudaLaunchKernelEx(&cfg, &grad_kernel<MT>, a, codes_map, dy_map);
     ctx->launches += 1;
     return cuda_status(e != cudaSuccess ? e : cudaGetLastError());
 }
@@ -220,7 +346,19 @@ int launch_project_grad(zipml_ctx* ctx, const GradArgs& in) {
     a.down_blocks = a.grad_down ? (a.inputs + 127) / 128 : 0;
     a.up_blocks = a.grad_up ? (a.outputs + 63) / 64 : 0;
     if (a.down_blocks + a.up_blocks == 0 || a.adapters == 0) return ZIPML_OK;
-    return a.rank <= 16 ? launch_grad_as<1>(ctx, a) : launch_grad_as<2>(ctx, a);
+    if (a.tokens > 0x7fffffffLL) return ZIPML_ERR_WORKSPACE;
+    CUtensorMap codes_map{}, dy_map{};
+    if (a.grad_down && a.tokens > 0) {
+        const int rc = encode_map(ctx, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.codes, a.code_stride, a.tokens, a.code_stride, 128, kGradChunk, CU_TENSOR_MAP_SWIZZLE_128B,
+                                  &codes_map);
+        if (rc != ZIPML_OK) return rc;
+    }
+    a.dy_copied = (reinterpret_cast<uintptr_t>(a.dy) & 15) == 0 && a.lddy % 8 == 0;
+    if (a.grad_up && a.tokens > 0 && a.dy_copied) {
+        const int rc = encode_map(ctx, CU_TENSOR_MAP_DATA_TYPE_UINT16, a.dy, a.outputs, a.tokens, a.lddy * 2, 64, kGradChunk, CU_TENSOR_MAP_SWIZZLE_128B, &dy_map);
+        if (rc != ZIPML_OK) return rc;
+    }
+    return a.rank <= 16 ? launch_grad_as<1>(ctx, a, codes_map, dy_map) : launch_grad_as<2>(ctx, a, codes_map, dy_map);
 }
 
 }  // namespace zipml

@@ -15,7 +15,7 @@ __device__ __forceinline__ unsigned long long global_ns() {
 
 // Waits for a phase of a shared-memory barrier; false, with ZIPML_ERR_TIMEOUT recorded, after kTcWaitNs, or once another thread
 // of the block has given up.
-__device__ __noinline__ bool tc_wait_long(uint64_t* bar, uint32_t parity, volatile int* gave_up, DeviceStatus* status, int where) {
+static __device__ __noinline__ bool tc_wait_long(uint64_t* bar, uint32_t parity, volatile int* gave_up, DeviceStatus* status, int where) {
     const unsigned long long began = global_ns();
     for (;;) {
 #pragma unroll 1
@@ -32,7 +32,7 @@ __device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, volatile
     return mbar_try_wait(bar, parity) || tc_wait_long(bar, parity, gave_up, status, where);
 }
 // The same for a block that has given up and still has copies or products in flight.
-__device__ __noinline__ void tc_drain(uint64_t* bar, uint32_t parity) {
+static __device__ __noinline__ void tc_drain(uint64_t* bar, uint32_t parity) {
     const unsigned long long began = global_ns();
     while (!mbar_try_wait(bar, parity) && global_ns() - began < kTcWaitNs) {}
 }
