@@ -5,6 +5,7 @@
 #include <cooperative_groups.h>
 
 #include "project.cuh"
+#include "tensor_core.cuh"
 
 namespace zipml {
 
@@ -235,6 +236,372 @@ __global__ void __launch_bounds__(32 * kShrinkWarps) shrink_kernel(ShrinkArgs a)
     cluster.sync();                                      // (no CTA leaves while another may still read its sums)
 }
 
+// ---------------------------------------------------------------------------------------------
+// Many tokens: tiles of 128 on the tensor cores' rows, the adapters' ranks on the columns, both operands by tensor copies.  What counts is
+// that the tokens' bytes keep coming (up to eight stages of 16 KB on their way), the products are next to nothing.  The forward pass's
+// sums are one more column: 16 rows of ones lead the right operand.  A tile's adapters take `slots` at a time; a column that does not belong to
+// a token's adapter, and ranks past the last that a copy's box brings along, are not read.  A cluster's CTAs divide the columns.
+// 8192 tokens x 8192 x 32 ranks: 200 us with the kernel above (its 16-byte loads left most of each turn waiting).
+// ---------------------------------------------------------------------------------------------
+constexpr int kTallTokens = 128;
+constexpr int kTallDepth = 64;
+constexpr int kTallThreads = 256;
+constexpr int kTallMostStages = 8;
+constexpr uint32_t kTallLeftBytes = kTallTokens * kTallDepth * 2;
+
+struct TallShared {
+    uint64_t full[kTallMostStages], empty[kTallMostStages], done;
+    uint32_t tmem;
+    int gave_up;
+    int ids[kTallTokens], distinct[kTallTokens], count;
+    float sum[kTallTokens];
+};
+
+struct TallShape {
+    int slots, ranks8, lead, rows, columns, stages;      // rows of the right operand; columns of tensor memory
+};
+
+template <bool BF16>
+__global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs a, TallShape f, const __grid_constant__ CUtensorMap z_map,
+                                                                      const __grid_constant__ CUtensorMap down_map) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    extern __shared__ uint8_t raw[];
+    uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    const uint32_t right_bytes = (uint32_t)f.rows * 128, stage_bytes = kTallLeftBytes + right_bytes;
+    float* part = reinterpret_cast<float*>(ring + f.stages * stage_bytes);            // [token][rank]
+    TallShared& sh = *reinterpret_cast<TallShared*>(part + kTallTokens * a.rank);
+    cg::cluster_group cluster = cg::this_cluster();
+    const int crank = (int)cluster.block_rank(), cranks = (int)cluster.num_blocks();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t t0 = (int64_t)(blockIdx.x / cranks) * kTallTokens;
+    const int all_steps = (a.columns + kTallDepth - 1) / kTallDepth, per = (all_steps + cranks - 1) / cranks;
+    const int step0 = min(crank * per, all_steps), steps = min(per, all_steps - step0);
+    volatile int* gave_up = &sh.gave_up;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kTallMostStages; ++i) {
+            mbar_init(&sh.full[i], 1);
+            mbar_init(&sh.empty[i], 1);
+        }
+        mbar_init(&sh.done, 1);
+        sh.gave_up = 0;
+        mbar_fence_init();
+    }
+    if (warp == 2) {
+        tc_alloc<false>(&sh.tmem, (uint32_t)f.columns);
+        tc_fence_before();
+    }
+    if (threadIdx.x < kTallTokens) {
+        sh.ids[threadIdx.x] = !a.starts && t0 + threadIdx.x < a.tokens ? -1 : kNoRequest;
+        sh.sum[threadIdx.x] = 0.0f;
+    }
+    for (int i = threadIdx.x; i < kTallTokens * a.rank; i += kTallThreads) part[i] = 0.0f;
+    // ones: bf16 0x3F80, fp16 0x3C00
+    for (int i = threadIdx.x; i < f.stages * f.lead * 8; i += kTallThreads) {
+        const uint32_t one = BF16 ? 0x3F803F80u : 0x3C003C00u;
+        *reinterpret_cast<uint4*>(ring + (i / (f.lead * 8)) * stage_bytes + kTallLeftBytes + (i % (f.lead * 8)) * 16) = make_uint4(one, one, one, one);
+    }
+    tc_publish();
+    __syncthreads();
+    tc_fence_after();
+    // the tokens' adapters, request by request
+    if (a.starts) {
+        for (int q = threadIdx.x; q < a.requests; q += kTallThreads) {
+            const int64_t s = max((int64_t)a.starts[q], t0), e = min(min((int64_t)a.starts[q + 1], a.tokens), t0 + kTallTokens);
+            if (s >= e) continue;
+            int id = a.which[q];
+            if (id >= a.adapters) {
+                set_status(a.status, ZIPML_ERR_INVALID_ARG, 91);
+                id = -1;
+            }
+            for (int64_t t = s; t < e; ++t) sh.ids[t - t0] = max(id, -1);
+        }
+        __syncthreads();
+    }
+    if (warp == 0) {
+        int mine[kTallTokens / 32], count = 0;
+#pragma unroll
+        for (int i = 0; i < kTallTokens / 32; ++i) mine[i] = f.slots > 0 ? sh.ids[lane + 32 * i] : -1;
+        for (;;) {
+            int least = 0x7fffffff;                                                   // (in the order of their numbers: every CTA of the cluster the same)
+#pragma unroll
+            for (int i = 0; i < kTallTokens / 32; ++i)
+                if (mine[i] >= 0) least = min(least, mine[i]);
+            least = __reduce_min_sync(0xffffffffu, least);
+            if (least == 0x7fffffff) break;
+#pragma unroll
+            for (int i = 0; i < kTallTokens / 32; ++i)
+                if (mine[i] == least) mine[i] = -1;
+            if (lane == 0) sh.distinct[count] = least;
+            ++count;
+        }
+        if (lane == 0) sh.count = count;
+    }
+    __syncthreads();
+    const uint32_t tmem = sh.tmem;
+    const int passes = max(f.slots > 0 ? (sh.count + f.slots - 1) / f.slots : 0, f.lead > 0 ? 1 : 0);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int n = 0;                                                                // stages of all passes
+            bool ok = true;
+            for (int p = 0; ok && p < passes; ++p) {
+                const int used = min(f.slots, sh.count - p * f.slots);
+                for (int s = 0; s < steps; ++s, ++n) {
+                    const int slot = n % f.stages;
+                    if (n >= f.stages && !tc_wait(&sh.empty[slot], (n / f.stages - 1) & 1, gave_up, a.status, 110)) { ok = false; break; }
+                    mbar_arrive_expect_tx(&sh.full[slot], kTallLeftBytes + (uint32_t)(max(used, 0) * f.ranks8 * 128));
+                    const uint32_t at = smem_u32(ring + slot * stage_bytes);
+                    tc_copy_2d(at, &z_map, (step0 + s) * kTallDepth, (int)t0, &sh.full[slot]);
+                    for (int i = 0; i < used; ++i)
+                        tc_copy_2d(at + kTallLeftBytes + (f.lead + i * f.ranks8) * 128, &down_map, (step0 + s) * kTallDepth, sh.distinct[p * f.slots + i] * a.rank, &sh.full[slot]);
+                }
+            }
+            if (!ok)
+                for (int i = max(0, n - f.stages); i < n; ++i) tc_drain(&sh.full[i % f.stages], (i / f.stages) & 1);
+        }
+    } else if (warp == 1) {
+        int n = 0;
+        bool ok = true;
+        const uint64_t z_at = tc_operand(smem_u32(ring), 16, 1024), d_at = tc_operand(smem_u32(ring + kTallLeftBytes), 16, 1024);
+        for (int p = 0; p < passes; ++p) {                                            // (every pass's barrier, whether or not a wait has given up)
+            const int used = max(min(f.slots, sh.count - p * f.slots), 0);
+            const uint32_t kind = tc_kind(BF16, false, kTallTokens, (f.lead + used * f.ranks8 + 15) & ~15);
+            // (the pass before has to have been read out of tensor memory)
+            if (p > 0) asm volatile("bar.sync 1, %0;" ::"n"(32 * 5) : "memory");
+            tc_fence_after();
+            for (int s = 0; ok && s < steps; ++s, ++n) {
+                const int slot = n % f.stages;
+                ok = __all_sync(0xffffffffu, tc_wait(&sh.full[slot], (n / f.stages) & 1, gave_up, a.status, 111));
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t offset = (uint64_t)((uint32_t)slot * (stage_bytes / 16));
+                if (tc_elect()) {
+#pragma unroll
+                    for (int k = 0; k < kTallDepth / 16; ++k) tc_mma<false>(tmem, z_at + offset + k * 2, d_at + offset + k * 2, kind, s > 0 || k > 0);
+                    tc_commit<false>(&sh.empty[slot]);
+                }
+                __syncwarp();
+            }
+            if (tc_elect()) tc_commit<false>(&sh.done);
+            __syncwarp();
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp - 4, row = quarter * 32 + lane, id = sh.ids[row];
+        bool ok = true;
+        for (int p = 0; p < passes; ++p) {
+            const int used = max(min(f.slots, sh.count - p * f.slots), 0);
+            ok = __all_sync(0xffffffffu, ok && tc_wait(&sh.done, p & 1, gave_up, a.status, 112));
+            if (ok && steps > 0) {
+                tc_fence_after();
+                const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16);
+                if (f.lead > 0 && p == 0) {
+                    uint32_t v[8];
+                    tc_load8(at, v);
+                    tc_load_wait();
+                    sh.sum[row] = __uint_as_float(v[0]);
+                }
+                for (int i = 0; i < used; ++i) {
+                    const bool mine = sh.distinct[p * f.slots + i] == id;
+                    for (int r = 0; r < f.ranks8; r += 8) {
+                        uint32_t v[8];
+                        tc_load8(at + f.lead + i * f.ranks8 + r, v);
+                        tc_load_wait();
+                        if (mine) {
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                if (r + k < a.rank) part[row * a.rank + r + k] = __uint_as_float(v[k]);
+                        }
+                    }
+                }
+                tc_fence_before();
+            }
+            if (p + 1 < passes) asm volatile("bar.sync 1, %0;" ::"n"(32 * 5) : "memory");
+        }
+    }
+    __syncthreads();
+    if (warp == 2) {
+        tc_fence_after();
+        tc_free<false>(tmem, (uint32_t)f.columns);
+    }
+    cluster.sync();
+    // the cluster's sums, a warp a token
+    for (int row = crank * (kTallThreads / 32) + warp; row < kTallTokens; row += cranks * (kTallThreads / 32)) {
+        const int64_t t = t0 + row;
+        const int id = sh.ids[row];
+        if (t >= a.tokens) continue;
+        if (f.slots > 0 && id != kNoRequest) {
+            const float scale = id >= 0 ? (a.scale ? a.scale[id] : 1.0f) : 0.0f;
+            float top = 0.0f;
+            for (int r = lane; r < a.rank; r += 32) {
+                float s = 0.0f;
+                if (id >= 0) {
+                    for (int c = 0; c < cranks; ++c) s += cluster.map_shared_rank(part, c)[row * a.rank + r];
+                    s *= scale;
+                }
+                a.hidden[t * a.rank + r] = s;
+                top = fmaxf(top, fabsf(s));
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            if (lane == 0) a.hidden_scale[t] = 1.0f / scale_to_range(top);
+        }
+        if (lane == 0) {
+            a.ids[t] = id;
+            if (f.lead > 0) {
+                float s = 0.0f;
+                for (int c = 0; c < cranks; ++c) s += cluster.map_shared_rank(sh.sum, c)[row];
+                a.sum[t] = id == kNoRequest ? 0.0f : s;
+            }
+        }
+    }
+    cluster.sync();
+}
+
+// ---------------------------------------------------------------------------------------------
+// The backward pass's rows: sum z mid and the largest |z step| of a row, then z step 2^k in fp16 (11 bits where bf16 would keep 8, one
+// rounding).  A CTA takes several rows, so that the grids' 8 bytes a column are read once for all of them; the second look at z finds it in
+// L1 or L2.  Bound by HBM: z once in, once out.
+// ---------------------------------------------------------------------------------------------
+constexpr int kScaleRows = 4;
+constexpr int kScaleThreads = 256;
+
+template <typename T>
+__global__ void __launch_bounds__(kScaleThreads) scale_rows_kernel(ShrinkArgs a) {
+    __shared__ float sums[kScaleRows][kScaleThreads / 32], tops[kScaleRows][kScaleThreads / 32];
+    const T* z = reinterpret_cast<const T*>(a.z);
+    const int64_t t0 = (int64_t)blockIdx.x * kScaleRows;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool wide = ((reinterpret_cast<uintptr_t>(z) | (uintptr_t)(a.ldz * 2)) & 15) == 0;
+    const bool wide_grid = ((reinterpret_cast<uintptr_t>(a.lo) | reinterpret_cast<uintptr_t>(a.step)) & 15) == 0;
+    const auto load_grid = [&](const float* p, int j, int count, float (&v)[8]) {
+        if (wide_grid && count == 8) {
+            const float4 x = *reinterpret_cast<const float4*>(p + j), y = *reinterpret_cast<const float4*>(p + j + 4);
+            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < count ? p[j + i] : 0.0f;
+        }
+    };
+    float sum[kScaleRows] = {}, top[kScaleRows] = {};
+    for (int j = threadIdx.x * 8; j < a.columns; j += kScaleThreads * 8) {
+        const int count = min(a.columns - j, 8);
+        uint4 w[kScaleRows];
+#pragma unroll
+        for (int r = 0; r < kScaleRows; ++r) w[r] = t0 + r < a.tokens ? load8_16(z + (t0 + r) * a.ldz + j, count, wide) : make_uint4(0, 0, 0, 0);
+        float lo[8], step[8];
+        load_grid(a.lo, j, count, lo);
+        load_grid(a.step, j, count, step);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lo[i] = fmaf(a.center, step[i], lo[i]);
+#pragma unroll
+        for (int r = 0; r < kScaleRows; ++r) {
+            const uint32_t u[4] = {w[r].x, w[r].y, w[r].z, w[r].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 v = unpack_pair<T>(u[i]);
+                sum[r] = fmaf(v.x, lo[2 * i], fmaf(v.y, lo[2 * i + 1], sum[r]));
+                top[r] = fmaxf(top[r], fmaxf(fabsf(v.x * step[2 * i]), fabsf(v.y * step[2 * i + 1])));
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < kScaleRows; ++r) {
+        sum[r] = warp_sum(sum[r]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], o));
+        if (lane == 0) { sums[r][warp] = sum[r]; tops[r][warp] = top[r]; }
+    }
+    __syncthreads();
+    float scale[kScaleRows];
+#pragma unroll
+    for (int r = 0; r < kScaleRows; ++r) {
+        float s = 0.0f, m = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kScaleThreads / 32; ++w) { s += sums[r][w]; m = fmaxf(m, tops[r][w]); }
+        scale[r] = scale_to_range(m);
+        if (threadIdx.x == 0 && t0 + r < a.tokens) { a.sum[t0 + r] = s; a.row_scale[t0 + r] = 1.0f / scale[r]; }
+    }
+    for (int j = threadIdx.x * 8; j < a.columns; j += kScaleThreads * 8) {
+        const int count = min(a.columns - j, 8);
+        float step[8];
+        load_grid(a.step, j, count, step);
+#pragma unroll
+        for (int r = 0; r < kScaleRows; ++r) {
+            if (t0 + r >= a.tokens) break;
+            const uint4 w = load8_16(z + (t0 + r) * a.ldz + j, count, wide);
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+            uint32_t o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 v = unpack_pair<T>(u[i]);
+                o[i] = pack_pair<__half>(v.x * step[2 * i] * scale[r], v.y * step[2 * i + 1] * scale[r]);
+            }
+            *reinterpret_cast<uint4*>(a.scaled + (t0 + r) * a.ld_scaled + j) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+    }
+}
+
+// Whether the kernel for many tokens takes them: rows that tensor copies can read, enough tokens to fill its tiles and few adapters in each.
+static bool tall_takes(const ShrinkArgs& a) {
+    if (a.tokens < 2 * kTallTokens || a.copy) return false;
+    if ((reinterpret_cast<uintptr_t>(a.z) & 15) || a.ldz % 8) return false;
+    if (a.down && ((reinterpret_cast<uintptr_t>(a.down) & 15) || a.columns % 8 || a.tokens < (int64_t)a.requests * 32)) return false;
+    return true;
+}
+
+static int launch_tall(zipml_ctx* ctx, const ShrinkArgs& a, int dtype, bool sums) {
+    TallShape f{};
+    f.lead = sums ? 16 : 0;
+    f.ranks8 = (a.rank + 7) / 8 * 8;
+    if (a.down) {
+        f.slots = f.ranks8 >= 64 ? 1 : 64 / f.ranks8;
+        if (f.slots > a.adapters) f.slots = a.adapters;
+        if (f.slots > a.requests) f.slots = a.requests;
+    }
+    f.rows = (f.lead + f.slots * f.ranks8 + 15) / 16 * 16;
+    f.columns = 32;
+    while (f.columns < f.rows) f.columns *= 2;
+    const size_t stage = kTallLeftBytes + (size_t)f.rows * 128, fixed = 1024 + sizeof(float) * kTallTokens * a.rank + sizeof(TallShared);
+    f.stages = (int)((200 * 1024 - fixed) / stage);
+    if (f.stages > kTallMostStages) f.stages = kTallMostStages;
+    const size_t smem = fixed + f.stages * stage;
+    const int64_t tiles = (a.tokens + kTallTokens - 1) / kTallTokens;
+    const int steps = (a.columns + kTallDepth - 1) / kTallDepth;
+    int ranks = 1;
+    while (ranks < 8 && tiles * ranks * 2 <= ctx->sm_count && steps / (ranks * 2) >= 4) ranks *= 2;
+    CUtensorMap z_map{}, down_map{};
+    const CUtensorMapDataType type = dtype == ZIPML_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    int rc = encode_map(ctx, type, a.z, a.columns, a.tokens, a.ldz * 2, kTallDepth, kTallTokens, CU_TENSOR_MAP_SWIZZLE_128B, &z_map);
+    if (rc == ZIPML_OK && a.down)
+        rc = encode_map(ctx, type, a.down, a.columns, (int64_t)a.adapters * a.rank, (int64_t)a.columns * 2, kTallDepth, f.ranks8, CU_TENSOR_MAP_SWIZZLE_128B, &down_map);
+    if (rc != ZIPML_OK) return rc;
+    auto kernel = dtype == ZIPML_BF16 ? &shrink_tall_kernel<true> : &shrink_tall_kernel<false>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return cuda_status(e);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(tiles * ranks));
+    cfg.blockDim = dim3(kTallThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = ctx->stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, kernel, a, f, z_map, down_map);
+    ctx->launches += 1;
+    return cuda_status(e != cudaSuccess ? e : cudaGetLastError());
+}
+
+static int launch_scale_rows(zipml_ctx* ctx, const ShrinkArgs& a, int dtype) {
+    const unsigned grid = (unsigned)((a.tokens + kScaleRows - 1) / kScaleRows);
+    if (dtype == ZIPML_BF16) scale_rows_kernel<__nv_bfloat16><<<grid, kScaleThreads, 0, ctx->stream>>>(a);
+    else scale_rows_kernel<__half><<<grid, kScaleThreads, 0, ctx->stream>>>(a);
+    ctx->launches += 1;
+    return cuda_status(cudaGetLastError());
+}
+
 template <typename T, bool BACK, int RT>
 static int launch_shrink_as(zipml_ctx* ctx, const ShrinkArgs& a) {
     const size_t smem = (size_t)kShrinkWarps * kShrinkRows * RT * 8 * sizeof(float);
@@ -277,6 +644,13 @@ static int launch_shrink_ranks(zipml_ctx* ctx, const ShrinkArgs& a) {
 }
 
 int launch_shrink(zipml_ctx* ctx, const ShrinkArgs& a, int dtype, bool backward) {
+    if (tall_takes(a)) {
+        if (backward && a.scaled) {
+            const int rc = launch_scale_rows(ctx, a, dtype);
+            if (rc != ZIPML_OK) return rc;
+        }
+        return launch_tall(ctx, a, dtype, !backward);
+    }
     if (dtype == ZIPML_BF16) return backward ? launch_shrink_ranks<__nv_bfloat16, true>(ctx, a) : launch_shrink_ranks<__nv_bfloat16, false>(ctx, a);
     return backward ? launch_shrink_ranks<__half, true>(ctx, a) : launch_shrink_ranks<__half, false>(ctx, a);
 }
