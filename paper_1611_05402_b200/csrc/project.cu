@@ -19,9 +19,10 @@ namespace cg = cooperative_groups;
 //             operand); backward: a code row is a feature (K-major).
 //   tokens    a tensor copy lays the right operand out itself.
 //   product   one thread issues 128 x NT x 16 four times, sums in tensor memory.
-// The adapters then take further stages of the same ring: up_i's rows are the left operand as they lie, hidden the right one, in two
-// 16-bit parts (high and low: 16 or more bits), zero for tokens of other adapters, over the 16-token window that holds i's tokens.  Their
-// sums have columns of their own, since the grids' steps do not apply to them.
+// The adapters then take further stages: the ranks of the tile's adapters, each padded to a multiple of 8, follow one another as a depth of
+// their own, 32 a stage.  up_i's rows are the left operand as they lie, hidden the right one, in two 16-bit parts (high and low: 16 or more
+// bits), zero for tokens of other adapters, over the 16-token windows that hold the stage's tokens.  Their sums have columns of their own,
+// since the grids' steps do not apply to them.
 // The epilogue takes steps, sums and scales together in fp32 and rounds once.  With few tokens a cluster's CTAs divide the depth and
 // add their results through each other's shared memory in a fixed order.
 // ---------------------------------------------------------------------------------------------
@@ -67,7 +68,8 @@ struct ProjShared {
     uint32_t tmem;
     int gave_up;
     int entries;                              // adapters of this tile that fall to this CTA
-    int entry_id[NT], entry_lo[NT], entry_n[NT];
+    int entry_id[NT], entry_lo[NT], entry_end[NT];
+    int entry[NT];                            // of a token, -1: none
 };
 
 // A slot of a ring and the parity of its current turn.
@@ -235,7 +237,22 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
     if constexpr (PAIR) cluster.sync();                               // (the other CTA's barriers and its tensor memory are there too)
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
-    const int chunks = a.up ? (a.rank + kRankChunk - 1) / kRankChunk : 0;
+    const int rank8 = a.up ? (a.rank + 7) & ~7 : 0;
+    // stages of the adapters' ranks, and the columns that stage j's tokens lie in (the first stage takes all, so that the others' sums start from
+    // zero, and so does every one of a pair's, which holds the operand's tokens in two places)
+    const auto up_stages = [&] { return (sh.entries * rank8 + kRankChunk - 1) / kRankChunk; };
+    const auto window = [&](int j, int& lo, int& n) {
+        lo = 0;
+        n = NT;
+        if (j == 0 || PAIR) return;
+        int end = 0;
+        lo = NT;
+        for (int e = j * kRankChunk / rank8; e < sh.entries && e * rank8 < (j + 1) * kRankChunk; ++e) {
+            lo = min(lo, sh.entry_lo[e]);
+            end = max(end, sh.entry_end[e]);
+        }
+        n = end - lo;
+    };
 
     if (warp == 0) {
         // the tokens' operand
@@ -295,7 +312,8 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 if (a.up && id >= 0) tok.hidden_scale = a.hidden_scale[t0 + t];
             }
             if (t < NT) sh.token[t] = tok;
-            mine[i] = chunks > 0 ? id : -1;
+            if (t < NT) sh.entry[t] = -1;
+            mine[i] = rank8 > 0 ? id : -1;
         }
         int found = 0, entries = 0;
         for (;;) {
@@ -311,21 +329,20 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 if (lane + 32 * i == first) id = mine[i];
             id = __shfl_sync(0xffffffffu, id, first & 31);
             int last = first;
+            const bool here = found++ % cranks == crank;
 #pragma unroll
             for (int i = 0; i < PER; ++i)
                 if (mine[i] == id) {
                     last = max(last, lane + 32 * i);
                     mine[i] = -1;
+                    if (here) sh.entry[lane + 32 * i] = entries;
                 }
             last = __reduce_max_sync(0xffffffffu, last);
-            if (found++ % cranks == crank) {
+            if (here) {
                 if (lane == 0) {
-                    // (the first one takes every column, so that the others' sums start from zero)
-                    // (and so does every one of a pair's, which holds the operand's tokens in two places)
-                    const int lo = entries == 0 || PAIR ? 0 : first & ~15;
                     sh.entry_id[entries] = id;
-                    sh.entry_lo[entries] = lo;
-                    sh.entry_n[entries] = entries == 0 || PAIR ? NT : (last + 16 - lo) & ~15;
+                    sh.entry_lo[entries] = first & ~15;
+                    sh.entry_end[entries] = (last + 16) & ~15;
                 }
                 ++entries;
             }
@@ -356,19 +373,20 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
         }
         if (tc_elect()) tc_commit<PAIR>(&sh.codes_done);
         __syncwarp();
-        if (ok && chunks > 0) ok = __all_sync(0xffffffffu, tc_wait(&sh.plan, 0, gave_up, a.status, 97));
-        if (ok && chunks > 0) {
-            const int count = sh.entries * chunks;
+        if (ok && rank8 > 0) ok = __all_sync(0xffffffffu, tc_wait(&sh.plan, 0, gave_up, a.status, 97));
+        if (ok && rank8 > 0) {
+            const int count = up_stages(), total = sh.entries * rank8;
             const uint64_t up_at = tc_operand(smem_u32(left), kLeftBytes / 2, 1024);
             for (int j = 0; j < count; ++j) {
-                const int slot = j % kGroups, e = j / chunks, c = j % chunks;
+                const int slot = j % kGroups;
                 ok = __all_sync(0xffffffffu, tc_wait(&sh.up_full[slot], (j / kGroups) & 1, gave_up, a.status, 98));
                 if (!ok) break;
                 tc_fence_after();
-                const int lo = sh.entry_lo[e];
+                int lo, n;
+                window(j, lo, n);
                 const uint64_t lp = up_at + (uint32_t)slot * (kLeftBytes / 16), rp = right_at + (uint32_t)slot * (Shape::kRightBytes / 16) + (uint32_t)lo * 8;
-                const uint32_t up_kind = tc_kind(BACK ? a.out_bf16 != 0 : BF16, true, kTileRows, sh.entry_n[e]);
-                const int ks = (min(kRankChunk, a.rank - c * kRankChunk) + 15) / 16;
+                const uint32_t up_kind = tc_kind(BACK ? a.out_bf16 != 0 : BF16, true, kTileRows, n);
+                const int ks = (min(kRankChunk, total - j * kRankChunk) + 15) / 16;
                 if (tc_elect()) {
                     for (int part = 0; part < 2; ++part)
                         for (int k = 0; k < ks; ++k)
@@ -422,28 +440,33 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             if (lane == 0) mbar_arrive(&sh.written[la.slot]);
         }
         if (ok) ok = __all_sync(0xffffffffu, tc_wait(&sh.plan, 0, gave_up, a.status, 101));
-        if (ok && chunks > 0) {
+        if (ok && rank8 > 0) {
             if (a.early) asm volatile("griddepcontrol.wait;" ::: "memory");
             const bool bf16 = BACK ? a.out_bf16 != 0 : BF16;
             const uint32_t exponent = bf16 ? 0x7f80u : 0x7c00u;
             const uint16_t* up = reinterpret_cast<const uint16_t*>(a.up);
             const bool wide = ((reinterpret_cast<uintptr_t>(up) | (uintptr_t)((int64_t)a.features * 2)) & 15) == 0;
             const bool wide_h = ((reinterpret_cast<uintptr_t>(a.hidden) | (uintptr_t)(a.rank * 4)) & 15) == 0;
-            const int entries = sh.entries;
+            const int entries = sh.entries, count = up_stages(), total = entries * rank8;
             bool bad = false;
             // Stages again, each group with a slot of its own.  An adapter's rows are on their way before the slot is free.
-            for (int j = group; ok && j < entries * chunks; j += kGroups) {
-                const int e = j / chunks, c = j % chunks, id = sh.entry_id[e];
-                const int rows = min(kRankChunk, a.rank - c * kRankChunk), padded = (rows + 15) & ~15;
+            for (int j = group; ok && j < count; j += kGroups) {
+                const int depth = min(kRankChunk, total - j * kRankChunk), padded = (depth + 15) & ~15;
                 constexpr int U = kRankChunk * 16 / kGroupThreads;
                 uint4 w[U];
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
-                    const int u = gid + i * kGroupThreads, k = u >> 4, f = f0 + (u & 15) * 8;
+                    const int u = gid + i * kGroupThreads, at = j * kRankChunk + (u >> 4), f = f0 + (u & 15) * 8, e = at / rank8, r = at - e * rank8;
                     w[i] = make_uint4(0, 0, 0, 0);
-                    if (k < rows) w[i] = load8_16(up + ((int64_t)id * a.rank + c * kRankChunk + k) * a.features + f, min(max(a.features - f, 0), 8), wide);
+                    if (e < entries && r < a.rank)
+                        w[i] = load8_16(up + ((int64_t)sh.entry_id[e] * a.rank + r) * a.features + f, min(max(a.features - f, 0), 8), wide);
                 }
-                const int lo = PAIR ? side * Shape::kRightRows : sh.entry_lo[e], n = PAIR ? Shape::kRightRows : sh.entry_n[e];
+                int lo, n;
+                window(j, lo, n);
+                if constexpr (PAIR) {
+                    lo = side * Shape::kRightRows;
+                    n = Shape::kRightRows;
+                }
                 const int per_row = padded >> 3, units = n * per_row;
                 constexpr int V = 2;                                       // units of 8 ranks of a token, on their way together
                 float v[V][8];
@@ -453,17 +476,19 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                         const int u = from + gid + i * kGroupThreads, t = lo + (per_row == 2 ? u >> 1 : u >> 2), chunk = u & (per_row - 1);
 #pragma unroll
                         for (int k = 0; k < 8; ++k) v[i][k] = 0.0f;
-                        if (u < units && sh.token[t].id == id) {
+                        if (u >= units) continue;
+                        const int at = j * kRankChunk + chunk * 8, e = at / rank8, r = at - e * rank8;
+                        if (sh.entry[t] == e) {
                             const float inv = 1.0f / sh.token[t].hidden_scale;     // (a power of two)
-                            const float* h = a.hidden + (t0 + t) * a.rank + c * kRankChunk + chunk * 8;
-                            if (wide_h && chunk * 8 + 8 <= rows) {
+                            const float* h = a.hidden + (t0 + t) * a.rank + r;
+                            if (wide_h && r + 8 <= a.rank) {
                                 const float4 x = *reinterpret_cast<const float4*>(h), y = *reinterpret_cast<const float4*>(h + 4);
                                 v[i][0] = x.x * inv; v[i][1] = x.y * inv; v[i][2] = x.z * inv; v[i][3] = x.w * inv;
                                 v[i][4] = y.x * inv; v[i][5] = y.y * inv; v[i][6] = y.z * inv; v[i][7] = y.w * inv;
                             } else {
 #pragma unroll
                                 for (int k = 0; k < 8; ++k)
-                                    if (chunk * 8 + k < rows) v[i][k] = h[k] * inv;
+                                    if (r + k < a.rank) v[i][k] = h[k] * inv;
                             }
                         }
                     }
@@ -528,7 +553,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 alpha = a.step[f];
                 beta = fmaf(a.center, alpha, a.lo[f]);
             }
-            const bool have_up = chunks > 0 && sh.entries > 0;
+            const bool have_up = sh.entries > 0;
             // A whole tile's rows pass through shared memory on their way out, so that a thread stores 16 bytes of a token's row.
             float* join = reinterpret_cast<float*>(ring);
             uint16_t* stage = reinterpret_cast<uint16_t*>(ring) + group * 2 * 16 * kProjRows;

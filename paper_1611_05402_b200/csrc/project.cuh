@@ -61,28 +61,6 @@ __device__ __forceinline__ float scale_to_range(float top) {
     return __uint_as_float((uint32_t)(min(max(13 - e, -126), 126) + 127) << 23);
 }
 
-// The request of token t: the last one that starts at or before it, -1 before the first, `requests` from the end on.
-__device__ __forceinline__ int request_of(const int32_t* starts, int requests, int64_t t) {
-    int lo = 0, hi = requests + 1;                                         // first index whose start is above t
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if ((int64_t)starts[mid] > t) hi = mid; else lo = mid + 1;
-    }
-    return lo - 1;
-}
-// Its adapter, kNoRequest outside the requests.  An index past the adapters counts as none and is reported.
-__device__ __forceinline__ int adapter_of(const int32_t* starts, const int32_t* which, int requests, int adapters, int64_t t, DeviceStatus* status) {
-    if (!starts) return -1;
-    const int q = request_of(starts, requests, t);
-    if (q < 0 || q >= requests) return kNoRequest;
-    const int i = which[q];
-    if (i >= adapters) {
-        set_status(status, ZIPML_ERR_INVALID_ARG, 91);
-        return -1;
-    }
-    return i < 0 ? -1 : i;
-}
-
 // Stage 1, over tokens x `columns` values z (the forward pass's inputs, the backward pass's output gradients):
 //   hidden[t] = scale_i * (D_i z_t)   D_i: rank x columns, the adapter of token t
 //   forward:  sum[t] = sum_j z_tj

@@ -41,6 +41,25 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
             : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// The adapters of the tile's tokens, request by request: all threads of a block, which is synchronised at the end.  A token that no request
+// holds has kNoRequest; an index past the adapters counts as none and is reported.
+template <int ROWS>
+__device__ __forceinline__ void find_adapters(const ShrinkArgs& a, int64_t t0, int* ids) {
+    if (threadIdx.x < ROWS) ids[threadIdx.x] = !a.starts && t0 + threadIdx.x < a.tokens ? -1 : kNoRequest;
+    __syncthreads();
+    if (a.starts) {
+        for (int q = threadIdx.x; q < a.requests; q += blockDim.x) {
+            const int which = a.which[q];                                             // (loaded with the others, not after them)
+            const int64_t s = max((int64_t)a.starts[q], t0), e = min(min((int64_t)a.starts[q + 1], a.tokens), t0 + ROWS);
+            if (s >= e) continue;
+            if (which >= a.adapters) set_status(a.status, ZIPML_ERR_INVALID_ARG, 91);
+            const int id = which >= a.adapters ? -1 : max(which, -1);
+            for (int64_t t = s; t < e; ++t) ids[t - t0] = id;
+        }
+        __syncthreads();
+    }
+}
+
 // RT: blocks of 8 ranks (0: no adapters).
 template <typename T, bool BACK, int RT>
 __global__ void __launch_bounds__(32 * kShrinkWarps) shrink_kernel(ShrinkArgs a) {
@@ -55,20 +74,18 @@ __global__ void __launch_bounds__(32 * kShrinkWarps) shrink_kernel(ShrinkArgs a)
     const int slice = blockIdx.y, slices = gridDim.y;     // this cluster's share of the tile's adapters
     constexpr int R = RT * 8;
 
-    if (threadIdx.x < kShrinkRows) {
-        const int64_t t = t0 + threadIdx.x;
-        sh.ids[threadIdx.x] = t < a.tokens ? adapter_of(a.starts, a.which, a.requests, a.adapters, t, a.status) : kNoRequest;
-    }
+    find_adapters<kShrinkRows>(a, t0, sh.ids);
     for (int i = threadIdx.x; i < kShrinkWarps * kShrinkRows * R; i += blockDim.x) part[i] = 0.0f;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        int count = 0, seen = 0;
-        for (int r = 0; r < kShrinkRows; ++r) {
-            bool fresh = sh.ids[r] >= 0;
-            for (int s = 0; s < r; ++s) fresh &= sh.ids[s] != sh.ids[r];
-            if (fresh && seen++ % slices == slice) sh.distinct[count++] = sh.ids[r];
-        }
-        sh.count = count;
+    if (warp == 0) {
+        // the first token of each adapter, and of those every slices-th
+        const int id = lane < kShrinkRows ? sh.ids[lane] : -1;
+        const uint32_t same = __match_any_sync(0xffffffffu, id);
+        const bool fresh = id >= 0 && (int)__ffs(same) - 1 == lane;
+        const uint32_t firsts = __ballot_sync(0xffffffffu, fresh);
+        const int nth = __popc(firsts & ((1u << lane) - 1u));
+        if (fresh && nth % slices == slice) sh.distinct[nth / slices] = id;
+        if (lane == 0) sh.count = (__popc(firsts) - slice + slices - 1) / slices;
     }
     __syncthreads();
 
@@ -291,10 +308,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
         tc_alloc<false>(&sh.tmem, (uint32_t)f.columns);
         tc_fence_before();
     }
-    if (threadIdx.x < kTallTokens) {
-        sh.ids[threadIdx.x] = !a.starts && t0 + threadIdx.x < a.tokens ? -1 : kNoRequest;
-        sh.sum[threadIdx.x] = 0.0f;
-    }
+    if (threadIdx.x < kTallTokens) sh.sum[threadIdx.x] = 0.0f;
     for (int i = threadIdx.x; i < kTallTokens * a.rank; i += kTallThreads) part[i] = 0.0f;
     // ones: bf16 0x3F80, fp16 0x3C00
     for (int i = threadIdx.x; i < f.stages * f.lead * 8; i += kTallThreads) {
@@ -304,20 +318,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
     tc_publish();
     __syncthreads();
     tc_fence_after();
-    // the tokens' adapters, request by request
-    if (a.starts) {
-        for (int q = threadIdx.x; q < a.requests; q += kTallThreads) {
-            const int64_t s = max((int64_t)a.starts[q], t0), e = min(min((int64_t)a.starts[q + 1], a.tokens), t0 + kTallTokens);
-            if (s >= e) continue;
-            int id = a.which[q];
-            if (id >= a.adapters) {
-                set_status(a.status, ZIPML_ERR_INVALID_ARG, 91);
-                id = -1;
-            }
-            for (int64_t t = s; t < e; ++t) sh.ids[t - t0] = max(id, -1);
-        }
-        __syncthreads();
-    }
+    find_adapters<kTallTokens>(a, t0, sh.ids);
     if (warp == 0) {
         int mine[kTallTokens / 32], count = 0;
 #pragma unroll
@@ -425,34 +426,35 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
         tc_free<false>(tmem, (uint32_t)f.columns);
     }
     cluster.sync();
-    // the cluster's sums, a warp a token
-    for (int row = crank * (kTallThreads / 32) + warp; row < kTallTokens; row += cranks * (kTallThreads / 32)) {
-        const int64_t t = t0 + row;
-        const int id = sh.ids[row];
-        if (t >= a.tokens) continue;
-        if (f.slots > 0 && id != kNoRequest) {
-            const float scale = id >= 0 ? (a.scale ? a.scale[id] : 1.0f) : 0.0f;
-            float top = 0.0f;
-            for (int r = lane; r < a.rank; r += 32) {
-                float s = 0.0f;
-                if (id >= 0) {
-                    for (int c = 0; c < cranks; ++c) s += cluster.map_shared_rank(part, c)[row * a.rank + r];
-                    s *= scale;
-                }
-                a.hidden[t * a.rank + r] = s;
-                top = fmaxf(top, fabsf(s));
+    // the cluster's sums: every CTA a block of the tokens, a thread a rank of one, then a thread a token
+    const int most = kTallTokens / cranks, row0 = crank * most;
+    if (f.slots > 0) {
+        for (int i = threadIdx.x; i < most * a.rank; i += kTallThreads) {
+            const int row = row0 + i / a.rank, id = sh.ids[row];
+            if (id == kNoRequest) continue;
+            float s = 0.0f;
+            if (id >= 0) {
+                for (int c = 0; c < cranks; ++c) s += cluster.map_shared_rank(part, c)[row0 * a.rank + i];
+                if (a.scale) s *= a.scale[id];
             }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            if (lane == 0) a.hidden_scale[t] = 1.0f / scale_to_range(top);
+            a.hidden[(t0 + row0) * a.rank + i] = s;
+            part[row0 * a.rank + i] = s;                                              // (no other CTA reads these)
         }
-        if (lane == 0) {
-            a.ids[t] = id;
-            if (f.lead > 0) {
-                float s = 0.0f;
-                for (int c = 0; c < cranks; ++c) s += cluster.map_shared_rank(sh.sum, c)[row];
-                a.sum[t] = id == kNoRequest ? 0.0f : s;
-            }
+        __syncthreads();
+    }
+    if ((int)threadIdx.x < most && t0 + row0 + (int)threadIdx.x < a.tokens) {
+        const int row = row0 + (int)threadIdx.x, id = sh.ids[row];
+        const int64_t t = t0 + row;
+        a.ids[t] = id;
+        if (f.slots > 0) {
+            float top = 0.0f;
+            for (int r = 0; r < a.rank; ++r) top = fmaxf(top, fabsf(part[row * a.rank + r]));
+            a.hidden_scale[t] = 1.0f / scale_to_range(id == kNoRequest ? 0.0f : top);
+        }
+        if (f.lead > 0) {
+            float s = 0.0f;
+            for (int c = 0; c < cranks; ++c) s += cluster.map_shared_rank(sh.sum, c)[row];
+            a.sum[t] = id == kNoRequest ? 0.0f : s;
         }
     }
     cluster.sync();
