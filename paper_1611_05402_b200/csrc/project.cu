@@ -238,6 +238,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
     const int rank8 = a.up ? (a.rank + 7) & ~7 : 0;
+    const uint32_t per_rank8 = rank8 > 0 ? 0xffffffffu / (uint32_t)rank8 + 1u : 0u;   // (place / rank8 as a high product: exact below 2^16)
     // stages of the adapters' ranks, and the columns that stage j's tokens lie in (the first stage takes all, so that the others' sums start from
     // zero, and so does every one of a pair's, which holds the operand's tokens in two places)
     const auto up_stages = [&] { return (sh.entries * rank8 + kRankChunk - 1) / kRankChunk; };
@@ -449,51 +450,56 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             const bool wide_h = ((reinterpret_cast<uintptr_t>(a.hidden) | (uintptr_t)(a.rank * 4)) & 15) == 0;
             const int entries = sh.entries, count = up_stages(), total = entries * rank8;
             bool bad = false;
-            // Stages again, each group with a slot of its own.  An adapter's rows are on their way before the slot is free.
-            for (int j = group; ok && j < count; j += kGroups) {
-                const int depth = min(kRankChunk, total - j * kRankChunk), padded = (depth + 15) & ~15;
-                constexpr int U = kRankChunk * 16 / kGroupThreads;
-                uint4 w[U];
+            // Stages again, each group with a slot of its own.  What a stage needs from global memory is on its way before its slot is free.
+            constexpr int U = kRankChunk * 16 / kGroupThreads, V = 2;      // units of 8 features of a rank, of 8 ranks of a token
+            uint4 w[U];
+            float v[V][8];
+            int lo = 0, units = 0, row_shift = 0;
+            const auto load_hidden = [&](int j, int from) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const int u = from + gid + i * kGroupThreads, t = lo + (u >> row_shift), at = j * kRankChunk + (u & ((1 << row_shift) - 1)) * 8;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[i][k] = 0.0f;
+                    if (u >= units) continue;
+                    const int e = (int)__umulhi((uint32_t)at, per_rank8), r = at - e * rank8;
+                    if (sh.entry[t] == e) {
+                        const float inv = 1.0f / sh.token[t].hidden_scale;         // (a power of two)
+                        const float* h = a.hidden + (t0 + t) * a.rank + r;
+                        if (wide_h && r + 8 <= a.rank) {
+                            const float4 x = *reinterpret_cast<const float4*>(h), y = *reinterpret_cast<const float4*>(h + 4);
+                            v[i][0] = x.x * inv; v[i][1] = x.y * inv; v[i][2] = x.z * inv; v[i][3] = x.w * inv;
+                            v[i][4] = y.x * inv; v[i][5] = y.y * inv; v[i][6] = y.z * inv; v[i][7] = y.w * inv;
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                if (r + k < a.rank) v[i][k] = h[k] * inv;
+                        }
+                    }
+                }
+            };
+            const auto load_stage = [&](int j) {
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
-                    const int u = gid + i * kGroupThreads, at = j * kRankChunk + (u >> 4), f = f0 + (u & 15) * 8, e = at / rank8, r = at - e * rank8;
+                    const int u = gid + i * kGroupThreads, at = j * kRankChunk + (u >> 4), f = f0 + (u & 15) * 8;
+                    const int e = (int)__umulhi((uint32_t)at, per_rank8), r = at - e * rank8;
                     w[i] = make_uint4(0, 0, 0, 0);
                     if (e < entries && r < a.rank)
                         w[i] = load8_16(up + ((int64_t)sh.entry_id[e] * a.rank + r) * a.features + f, min(max(a.features - f, 0), 8), wide);
                 }
-                int lo, n;
+                int n;
                 window(j, lo, n);
                 if constexpr (PAIR) {
                     lo = side * Shape::kRightRows;
                     n = Shape::kRightRows;
                 }
-                const int per_row = padded >> 3, units = n * per_row;
-                constexpr int V = 2;                                       // units of 8 ranks of a token, on their way together
-                float v[V][8];
-                const auto load = [&](int from) {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const int u = from + gid + i * kGroupThreads, t = lo + (per_row == 2 ? u >> 1 : u >> 2), chunk = u & (per_row - 1);
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) v[i][k] = 0.0f;
-                        if (u >= units) continue;
-                        const int at = j * kRankChunk + chunk * 8, e = at / rank8, r = at - e * rank8;
-                        if (sh.entry[t] == e) {
-                            const float inv = 1.0f / sh.token[t].hidden_scale;     // (a power of two)
-                            const float* h = a.hidden + (t0 + t) * a.rank + r;
-                            if (wide_h && r + 8 <= a.rank) {
-                                const float4 x = *reinterpret_cast<const float4*>(h), y = *reinterpret_cast<const float4*>(h + 4);
-                                v[i][0] = x.x * inv; v[i][1] = x.y * inv; v[i][2] = x.z * inv; v[i][3] = x.w * inv;
-                                v[i][4] = y.x * inv; v[i][5] = y.y * inv; v[i][6] = y.z * inv; v[i][7] = y.w * inv;
-                            } else {
-#pragma unroll
-                                for (int k = 0; k < 8; ++k)
-                                    if (r + k < a.rank) v[i][k] = h[k] * inv;
-                            }
-                        }
-                    }
-                };
-                load(0);
+                row_shift = total - j * kRankChunk > 16 ? 2 : 1;           // (a stage's depth counts as 16 or 32)
+                units = n << row_shift;
+                load_hidden(j, 0);
+            };
+            if (group < count) load_stage(group);
+            for (int j = group; ok && j < count; j += kGroups) {
+                const int padded = 8 << row_shift;
                 ok = j < kGroups ? tc_wait(&sh.codes_done, 0, gave_up, a.status, 102)
                                  : tc_wait(&sh.up_empty[group], (j / kGroups - 1) & 1, gave_up, a.status, 105);
                 ok = __all_sync(0xffffffffu, ok);
@@ -509,10 +515,10 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 }
                 uint8_t* tok = right + group * Shape::kRightBytes;
                 for (int from = 0; from < units; from += V * kGroupThreads) {
-                    if (from > 0) load(from);
+                    if (from > 0) load_hidden(j, from);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        const int u = from + gid + i * kGroupThreads, t = lo + (per_row == 2 ? u >> 1 : u >> 2), chunk = u & (per_row - 1);
+                        const int u = from + gid + i * kGroupThreads, t = lo + (u >> row_shift), chunk = u & ((1 << row_shift) - 1);
                         if (u >= units) continue;
                         uint32_t high[4], low[4];
 #pragma unroll
@@ -538,6 +544,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                     if (PAIR && side != 0) tc_arrive_at(tc_peer(&sh.up_full[group], 0));
                     else mbar_arrive(&sh.up_full[group]);
                 }
+                if (j + kGroups < count) load_stage(j + kGroups);
             }
             if (bad) set_status(a.status, ZIPML_ERR_NONFINITE, 103);
         }
