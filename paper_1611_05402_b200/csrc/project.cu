@@ -32,7 +32,8 @@ constexpr int kGroups = 3;                    // groups of unpacking warps, each
 constexpr int kGroupWarps = 4;
 constexpr int kGroupThreads = 32 * kGroupWarps;
 constexpr int kFirstPublisher = 4 + kGroups * kGroupWarps;     // a warp for each group
-constexpr int kProjThreads = 32 * (kFirstPublisher + kGroups);
+constexpr int kSecondIssuer = kFirstPublisher + kGroups;
+constexpr int kProjThreads = 32 * (kSecondIssuer + 1);
 constexpr int kMostSlots = 12;
 constexpr int kRankChunk = 32;                // ranks of an adapter stage: high parts in the first half of the depth, low ones in the second
 constexpr uint32_t kLeftBytes = kProjRows * kProjDepth * 2;
@@ -52,7 +53,12 @@ struct ProjShape {
     static constexpr uint32_t kCodeRing = (NT >= 128 ? 6 : NT == 64 ? 9 : 12) * kProjRows * kProjDepth;     // bytes for packed codes
     static_assert(kRight >= kGroups && kRight <= kLeft && kLeft % kGroups == 0 && kMostSlots % kGroups == 0, "slots by group");
     static constexpr uint32_t kRing = kLeft * kLeftBytes + kRight * kRightBytes + kCodeRing;
-    static constexpr uint32_t kColumns = NT == 16 ? 32 : 2 * NT;        // tensor memory: codes' sums, then adapters'
+    // Tensor memory: the codes' sums of each issuing warp, then the adapters'.  Two warps issue where products are small: a turn's own
+    // instructions, one after the other, take some 400 cycles, the products of 64 tokens 130.
+    static constexpr int kIssuers = PAIR ? 1 : 2;
+    static constexpr uint32_t kUpAt = kIssuers * NT;
+    static constexpr uint32_t kColumns = PAIR || NT == 128 ? 512 : NT == 64 ? 256 : 64;
+    static constexpr int kWindows = PAIR ? 1 : 4 * NT;                   // stages of adapters at most, for their windows
 };
 
 struct ProjToken {                            // what the epilogue needs of a token
@@ -60,7 +66,7 @@ struct ProjToken {                            // what the epilogue needs of a to
     int id;
 };
 
-template <int NT>
+template <int NT, bool PAIR>
 struct ProjShared {
     ProjToken token[NT];
     uint64_t codes_full[kMostSlots], codes_empty[kMostSlots], written[2 * kGroups], full[2 * kGroups], empty[2 * kGroups];
@@ -70,6 +76,7 @@ struct ProjShared {
     int entries;                              // adapters of this tile that fall to this CTA
     int entry_id[NT], entry_lo[NT], entry_end[NT];
     int entry[NT];                            // of a token, -1: none
+    uint16_t window_lo[ProjShape<NT, PAIR>::kWindows], window_n[ProjShape<NT, PAIR>::kWindows];
 };
 
 // A slot of a ring and the parity of its current turn.
@@ -188,7 +195,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
     constexpr int L = Shape::kLeft, R = Shape::kRight;
     extern __shared__ uint8_t raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-    ProjShared<NT>& sh = *reinterpret_cast<ProjShared<NT>*>(ring + Shape::kRing);
+    ProjShared<NT, PAIR>& sh = *reinterpret_cast<ProjShared<NT, PAIR>*>(ring + Shape::kRing);
     uint8_t* const left = ring;
     uint8_t* const right = ring + L * kLeftBytes;
     uint8_t* const packed = right + R * Shape::kRightBytes;
@@ -223,7 +230,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             mbar_init(&sh.up_full[i], (PAIR ? 2 : 1) * kGroupWarps);
             mbar_init(&sh.up_empty[i], 1);
         }
-        mbar_init(&sh.codes_done, 1);
+        mbar_init(&sh.codes_done, Shape::kIssuers);
         mbar_init(&sh.done, 1);
         mbar_init(&sh.plan, 32);
         sh.gave_up = 0;
@@ -239,21 +246,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
     const uint32_t tmem = sh.tmem;
     const int rank8 = a.up ? (a.rank + 7) & ~7 : 0;
     const uint32_t per_rank8 = rank8 > 0 ? 0xffffffffu / (uint32_t)rank8 + 1u : 0u;   // (place / rank8 as a high product: exact below 2^16)
-    // stages of the adapters' ranks, and the columns that stage j's tokens lie in (the first stage takes all, so that the others' sums start from
-    // zero, and so does every one of a pair's, which holds the operand's tokens in two places)
-    const auto up_stages = [&] { return (sh.entries * rank8 + kRankChunk - 1) / kRankChunk; };
-    const auto window = [&](int j, int& lo, int& n) {
-        lo = 0;
-        n = NT;
-        if (j == 0 || PAIR) return;
-        int end = 0;
-        lo = NT;
-        for (int e = j * kRankChunk / rank8; e < sh.entries && e * rank8 < (j + 1) * kRankChunk; ++e) {
-            lo = min(lo, sh.entry_lo[e]);
-            end = max(end, sh.entry_end[e]);
-        }
-        n = end - lo;
-    };
+    const auto up_stages = [&] { return (sh.entries * rank8 + kRankChunk - 1) / kRankChunk; };      // of the adapters' ranks
 
     if (warp == 0) {
         // the tokens' operand
@@ -348,62 +341,79 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 ++entries;
             }
         }
+        __syncwarp();
+        // The columns that a stage's tokens lie in.  The first stage takes all, so that the others' sums start from zero (and so does every one
+        // of a pair's, which holds the operand's tokens in two places).
+        if constexpr (!PAIR)
+            for (int j = lane; j * kRankChunk < entries * rank8; j += 32) {
+                int lo = j == 0 ? 0 : NT, end = j == 0 ? NT : 0;
+                for (int e = j * kRankChunk / rank8; j > 0 && e < entries && e * rank8 < (j + 1) * kRankChunk; ++e) {
+                    lo = min(lo, sh.entry_lo[e]);
+                    end = max(end, sh.entry_end[e]);
+                }
+                sh.window_lo[j] = (uint16_t)lo;
+                sh.window_n[j] = (uint16_t)(end - lo);
+            }
         if (lane == 0) sh.entries = entries;
         __syncwarp();
         mbar_arrive(&sh.plan);
-    } else if (warp == 1) {
-        // the products: the warp waits as a whole, one lane issues; of a pair, the first CTA's
-        if (side == 0) {
-        bool ok = true;
-        RingAt la, ra;
-        const uint32_t kind = tc_kind(BF16, !BACK, kTileRows, NT);
-        // (operands by their first slot: an address in steps of 16 bytes is the description's lowest field)
-        const uint64_t left_at = BACK ? tc_operand(smem_u32(left), 16, 1024) : tc_operand(smem_u32(left), kLeftBytes / 2, 1024);
-        const uint64_t right_at = tc_operand(smem_u32(right), 16, 1024);
-        for (int s = 0; s < steps; ++s, la.next(1, L), ra.next(1, R)) {
-            ok = __all_sync(0xffffffffu, tc_wait(&sh.full[la.slot], la.turn, gave_up, a.status, 95));
-            if (!ok) break;
-            tc_fence_after();
-            const uint64_t lp = left_at + (uint32_t)la.slot * (kLeftBytes / 16), rp = right_at + (uint32_t)ra.slot * (Shape::kRightBytes / 16);
-            if (tc_elect()) {
-#pragma unroll
-                for (int k = 0; k < kProjDepth / 16; ++k) tc_mma<PAIR>(tmem, lp + k * (BACK ? 2 : 128), rp + k * 2, kind, s > 0 || k > 0);
-                tc_commit<PAIR>(&sh.empty[la.slot]);
-            }
-            __syncwarp();
-        }
-        if (tc_elect()) tc_commit<PAIR>(&sh.codes_done);
-        __syncwarp();
-        if (ok && rank8 > 0) ok = __all_sync(0xffffffffu, tc_wait(&sh.plan, 0, gave_up, a.status, 97));
-        if (ok && rank8 > 0) {
-            const int count = up_stages(), total = sh.entries * rank8;
-            const uint64_t up_at = tc_operand(smem_u32(left), kLeftBytes / 2, 1024);
-            for (int j = 0; j < count; ++j) {
-                const int slot = j % kGroups;
-                ok = __all_sync(0xffffffffu, tc_wait(&sh.up_full[slot], (j / kGroups) & 1, gave_up, a.status, 98));
+    } else if (warp == 1 || warp == kSecondIssuer) {
+        // The products: a warp waits as a whole, one lane issues.  Two warps take every other stage, each into sums of its own; the first takes
+        // the adapters' stages too.  Of a pair, the first CTA's first warp.
+        const int issuer = warp == 1 ? 0 : 1;
+        if (side == 0 && issuer < Shape::kIssuers) {
+            bool ok = true;
+            RingAt la, ra;
+            la.next(issuer, L);
+            ra.next(issuer, R);
+            const uint32_t kind = tc_kind(BF16, !BACK, kTileRows, NT), sums = tmem + issuer * NT;
+            // (operands by their first slot: an address in steps of 16 bytes is the description's lowest field)
+            const uint64_t left_at = BACK ? tc_operand(smem_u32(left), 16, 1024) : tc_operand(smem_u32(left), kLeftBytes / 2, 1024);
+            const uint64_t right_at = tc_operand(smem_u32(right), 16, 1024);
+            for (int s = issuer; s < steps; s += Shape::kIssuers, la.next(Shape::kIssuers, L), ra.next(Shape::kIssuers, R)) {
+                ok = __all_sync(0xffffffffu, tc_wait(&sh.full[la.slot], la.turn, gave_up, a.status, 95));
                 if (!ok) break;
                 tc_fence_after();
-                int lo, n;
-                window(j, lo, n);
-                const uint64_t lp = up_at + (uint32_t)slot * (kLeftBytes / 16), rp = right_at + (uint32_t)slot * (Shape::kRightBytes / 16) + (uint32_t)lo * 8;
-                const uint32_t up_kind = tc_kind(BACK ? a.out_bf16 != 0 : BF16, true, kTileRows, n);
-                const int ks = (min(kRankChunk, total - j * kRankChunk) + 15) / 16;
+                const uint64_t lp = left_at + (uint32_t)la.slot * (kLeftBytes / 16), rp = right_at + (uint32_t)ra.slot * (Shape::kRightBytes / 16);
                 if (tc_elect()) {
-                    for (int part = 0; part < 2; ++part)
-                        for (int k = 0; k < ks; ++k)
-                            tc_mma<PAIR>(tmem + Shape::kColumns / 2 + lo, lp + k * 128, rp + part * 4 + k * 2, up_kind, j > 0 || part > 0 || k > 0);
-                    tc_commit<PAIR>(&sh.up_empty[slot]);
+#pragma unroll
+                    for (int k = 0; k < kProjDepth / 16; ++k) tc_mma<PAIR>(sums, lp + k * (BACK ? 2 : 128), rp + k * 2, kind, s > issuer || k > 0);
+                    tc_commit<PAIR>(&sh.empty[la.slot]);
                 }
                 __syncwarp();
             }
+            if (tc_elect()) tc_commit<PAIR>(&sh.codes_done);
+            __syncwarp();
+            if (issuer == 0) {
+                if (ok && rank8 > 0) ok = __all_sync(0xffffffffu, tc_wait(&sh.plan, 0, gave_up, a.status, 97));
+                if (ok && rank8 > 0) {
+                    const int count = up_stages(), total = sh.entries * rank8;
+                    const uint64_t up_at = tc_operand(smem_u32(left), kLeftBytes / 2, 1024);
+                    for (int j = 0, slot = 0, turn = 0; j < count; ++j) {
+                        ok = __all_sync(0xffffffffu, tc_wait(&sh.up_full[slot], turn, gave_up, a.status, 98));
+                        if (!ok) break;
+                        tc_fence_after();
+                        const int lo = PAIR ? 0 : sh.window_lo[j], n = PAIR ? NT : sh.window_n[j];
+                        const uint64_t lp = up_at + (uint32_t)slot * (kLeftBytes / 16), rp = right_at + (uint32_t)slot * (Shape::kRightBytes / 16) + (uint32_t)lo * 8;
+                        const uint32_t up_kind = tc_kind(BACK ? a.out_bf16 != 0 : BF16, true, kTileRows, n);
+                        const int ks = (min(kRankChunk, total - j * kRankChunk) + 15) / 16;
+                        if (tc_elect()) {
+                            for (int part = 0; part < 2; ++part)
+                                for (int k = 0; k < ks; ++k)
+                                    tc_mma<PAIR>(tmem + Shape::kUpAt + lo, lp + k * 128, rp + part * 4 + k * 2, up_kind, j > 0 || part > 0 || k > 0);
+                            tc_commit<PAIR>(&sh.up_empty[slot]);
+                        }
+                        __syncwarp();
+                        if (++slot == kGroups) { slot = 0; turn ^= 1; }
+                    }
+                }
+                if (tc_elect()) tc_commit<PAIR>(&sh.done);
+                __syncwarp();
+            }
+            if (!ok && lane == 0) tc_drain(issuer == 0 ? &sh.done : &sh.codes_done, 0);
+            __syncwarp();
         }
-        if (tc_elect()) {
-            tc_commit<PAIR>(&sh.done);
-            if (!ok) tc_drain(&sh.done, 0);
-        }
-        __syncwarp();
-        }
-    } else if (warp >= kFirstPublisher) {
+    } else if (warp >= kFirstPublisher && warp < kSecondIssuer) {
         // A group's stores, made visible to the tensor cores by a warp that has nothing else to do: the fence waits for what is on its way to
         // shared memory, 500 to 1,400 cycles beside running products, which the unpacking warps spent idle.
         RingAt la;
@@ -419,6 +429,13 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
         }
     } else {
         const int group = (warp - 4) / kGroupWarps, gid = (threadIdx.x - 128) % kGroupThreads;
+        // the epilogue's feature of this lane (a group's warps take 32 rows of tensor memory each) and its grid
+        const int row = (warp & 3) * 32 + lane, feature = f0 + row;
+        float alpha = 1.0f, beta = 1.0f;
+        if (a.step && feature < a.features) {
+            alpha = a.step[feature];
+            beta = fmaf(a.center, alpha, a.lo[feature]);
+        }
         int s = group;
         bool ok = true;
         RingAt ca, la;
@@ -464,16 +481,15 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                     if (u >= units) continue;
                     const int e = (int)__umulhi((uint32_t)at, per_rank8), r = at - e * rank8;
                     if (sh.entry[t] == e) {
-                        const float inv = 1.0f / sh.token[t].hidden_scale;         // (a power of two)
                         const float* h = a.hidden + (t0 + t) * a.rank + r;
                         if (wide_h && r + 8 <= a.rank) {
                             const float4 x = *reinterpret_cast<const float4*>(h), y = *reinterpret_cast<const float4*>(h + 4);
-                            v[i][0] = x.x * inv; v[i][1] = x.y * inv; v[i][2] = x.z * inv; v[i][3] = x.w * inv;
-                            v[i][4] = y.x * inv; v[i][5] = y.y * inv; v[i][6] = y.z * inv; v[i][7] = y.w * inv;
+                            v[i][0] = x.x; v[i][1] = x.y; v[i][2] = x.z; v[i][3] = x.w;
+                            v[i][4] = y.x; v[i][5] = y.y; v[i][6] = y.z; v[i][7] = y.w;
                         } else {
 #pragma unroll
                             for (int k = 0; k < 8; ++k)
-                                if (r + k < a.rank) v[i][k] = h[k] * inv;
+                                if (r + k < a.rank) v[i][k] = h[k];
                         }
                     }
                 }
@@ -487,12 +503,8 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                     if (e < entries && r < a.rank)
                         w[i] = load8_16(up + ((int64_t)sh.entry_id[e] * a.rank + r) * a.features + f, min(max(a.features - f, 0), 8), wide);
                 }
-                int n;
-                window(j, lo, n);
-                if constexpr (PAIR) {
-                    lo = side * Shape::kRightRows;
-                    n = Shape::kRightRows;
-                }
+                lo = PAIR ? side * Shape::kRightRows : sh.window_lo[j];
+                const int n = PAIR ? Shape::kRightRows : sh.window_n[j];
                 row_shift = total - j * kRankChunk > 16 ? 2 : 1;           // (a stage's depth counts as 16 or 32)
                 units = n << row_shift;
                 load_hidden(j, 0);
@@ -514,29 +526,30 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                     *reinterpret_cast<uint4*>(dst + (chunk >> 3) * (kLeftBytes / 2) + k * 128 + (((chunk & 7) ^ (k & 7)) << 4)) = w[i];
                 }
                 uint8_t* tok = right + group * Shape::kRightBytes;
-                for (int from = 0; from < units; from += V * kGroupThreads) {
-                    if (from > 0) load_hidden(j, from);
+                const auto store_hidden = [&](auto type, int from) {
+                    using T = decltype(type);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         const int u = from + gid + i * kGroupThreads, t = lo + (u >> row_shift), chunk = u & ((1 << row_shift) - 1);
                         if (u >= units) continue;
+                        const float inv = 1.0f / sh.token[t].hidden_scale;         // (a power of two)
                         uint32_t high[4], low[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            if (bf16) {
-                                high[k] = pack_pair<__nv_bfloat16>(v[i][2 * k], v[i][2 * k + 1]);
-                                const float2 f = unpack_pair<__nv_bfloat16>(high[k]);
-                                low[k] = pack_pair<__nv_bfloat16>(v[i][2 * k] - f.x, v[i][2 * k + 1] - f.y);
-                            } else {
-                                high[k] = pack_pair<__half>(v[i][2 * k], v[i][2 * k + 1]);
-                                const float2 f = unpack_pair<__half>(high[k]);
-                                low[k] = pack_pair<__half>(v[i][2 * k] - f.x, v[i][2 * k + 1] - f.y);
-                            }
+                            const float x = v[i][2 * k] * inv, y = v[i][2 * k + 1] * inv;
+                            high[k] = pack_pair<T>(x, y);
+                            const float2 f = unpack_pair<T>(high[k]);
+                            low[k] = pack_pair<T>(x - f.x, y - f.y);
                         }
                         uint8_t* p = tok + (PAIR ? t - lo : t) * 128;
                         *reinterpret_cast<uint4*>(p + ((chunk ^ (t & 7)) << 4)) = make_uint4(high[0], high[1], high[2], high[3]);
                         *reinterpret_cast<uint4*>(p + (((chunk + 4) ^ (t & 7)) << 4)) = make_uint4(low[0], low[1], low[2], low[3]);
                     }
+                };
+                for (int from = 0; from < units; from += V * kGroupThreads) {
+                    if (from > 0) load_hidden(j, from);
+                    if (bf16) store_hidden(__nv_bfloat16(), from);
+                    else store_hidden(__half(), from);
                 }
                 tc_publish();
                 __syncwarp();
@@ -548,62 +561,69 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             }
             if (bad) set_status(a.status, ZIPML_ERR_NONFINITE, 103);
         }
-        if (ok) ok = __all_sync(0xffffffffu, tc_wait(&sh.done, 0, gave_up, a.status, 104));
+        if (ok) ok = __all_sync(0xffffffffu, tc_wait(&sh.codes_done, 0, gave_up, a.status, 109) && tc_wait(&sh.done, 0, gave_up, a.status, 104));
         if (ok) {
             tc_fence_after();
-            // a group's warps take 32 rows of tensor memory each, the groups every third 16 tokens
-            const int quarter = warp & 3;
-            const int row = quarter * 32 + lane, f = f0 + row;
-            const bool in = f < a.features;
-            float alpha = 1.0f, beta = 1.0f;
-            if (a.step && in) {
-                alpha = a.step[f];
-                beta = fmaf(a.center, alpha, a.lo[f]);
-            }
-            const bool have_up = sh.entries > 0;
-            // A whole tile's rows pass through shared memory on their way out, so that a thread stores 16 bytes of a token's row.
-            float* join = reinterpret_cast<float*>(ring);
-            uint16_t* stage = reinterpret_cast<uint16_t*>(ring) + group * 2 * 16 * kProjRows;
-            const bool wide_out = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * 2)) & 15) == 0;
-            uint32_t v[16], w[16];
-            const uint32_t lanes_at = tmem + ((uint32_t)(quarter * 32) << 16);
+            // The groups take every third 16 tokens.  A whole tile's rows pass through shared memory on their way out, so that a thread stores 16
+            // bytes of a token's row; rows that are not aligned for that go out as they lie, 32 features a warp.
+            const bool have_up = sh.entries > 0, wide_out = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * 2)) & 15) == 0;
+            if (crank != 0) beta = 0.0f;
+            const uint32_t lanes_at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+            uint32_t v[16] = {}, v2[Shape::kIssuers == 2 ? 16 : 1] = {}, w[16] = {};
             const auto load = [&](int c) {
                 if (steps > 0) tc_load16(lanes_at + c * 16, v);
-                if (have_up) tc_load16(lanes_at + Shape::kColumns / 2 + c * 16, w);
+                if constexpr (Shape::kIssuers == 2)
+                    if (steps > 1) tc_load16(lanes_at + NT + c * 16, v2);
+                if (have_up) tc_load16(lanes_at + Shape::kUpAt + c * 16, w);
             };
-            if (group < NT / 16) load(group);
-            for (int c = group; c < NT / 16; c += kGroups) {
-                tc_load_wait();
+            // MODE 0: into the cluster's exchange, 1: staged, 2: straight out
+            const auto finish = [&](auto type, auto mode) {
+                using T = decltype(type);
+                constexpr int MODE = decltype(mode)::value;
+                float* join = reinterpret_cast<float*>(ring) + row;
+                T* stages = reinterpret_cast<T*>(ring) + group * 2 * 16 * kProjRows;
+                int turn = 0;
+                if (group < NT / 16) load(group);
+                for (int c = group; c < NT / 16; c += kGroups, turn ^= 1) {
+                    T* stage = stages + turn * 16 * kProjRows;            // (two buffers in turn: the next barrier tells that this one has been read)
+                    tc_load_wait();
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const ProjToken tok = sh.token[c * 16 + i];
-                    float y = crank == 0 ? beta * tok.sum : 0.0f;
-                    if (steps > 0) y = fmaf(alpha * tok.row_scale, __uint_as_float(v[i]), y);
-                    if (have_up && tok.id >= 0) y = fmaf(tok.hidden_scale, __uint_as_float(w[i]), y);
-                    if (cranks > 1) join[(c * 16 + i) * kProjRows + row] = y;
-                    else stage[i * kProjRows + row] = a.out_bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(y)) : __half_as_ushort(__float2half_rn(y));
-                }
-                if (c + kGroups < NT / 16) load(c + kGroups);             // (on its way while these rows go out)
-                if (cranks == 1) {
-                    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(kGroupThreads) : "memory");
+                    for (int i = 0; i < 16; ++i) {
+                        const ProjToken tok = sh.token[c * 16 + i];
+                        float sum = __uint_as_float(v[i]);
+                        if constexpr (Shape::kIssuers == 2) sum += __uint_as_float(v2[i]);
+                        const float y = fmaf(alpha * tok.row_scale, sum, fmaf(tok.hidden_scale, __uint_as_float(w[i]), beta * tok.sum));
+                        if constexpr (MODE == 0) join[(c * 16 + i) * kProjRows] = y;
+                        else if constexpr (MODE == 1) stage[i * kProjRows + row] = from_float<T>(y);
+                        else if (tok.id != kNoRequest && feature < a.features) reinterpret_cast<T*>(a.out)[(t0 + c * 16 + i) * a.ldo + feature] = from_float<T>(y);
+                    }
+                    if (c + kGroups < NT / 16) load(c + kGroups);         // (on its way while these rows go out)
+                    if constexpr (MODE == 1) {
+                        asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(kGroupThreads) : "memory");
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int u = gid + i * kGroupThreads, t = c * 16 + (u >> 4), at = f0 + (u & 15) * 8;
-                        if (sh.token[t].id == kNoRequest || at >= a.features) continue;
-                        const uint4 y = *reinterpret_cast<const uint4*>(stage + (u >> 4) * kProjRows + (u & 15) * 8);
-                        uint16_t* p = reinterpret_cast<uint16_t*>(a.out) + (t0 + t) * a.ldo + at;
-                        if (wide_out && at + 8 <= a.features) *reinterpret_cast<uint4*>(p) = y;
-                        else {
-                            const uint32_t e[4] = {y.x, y.y, y.z, y.w};
+                        for (int i = 0; i < 2; ++i) {
+                            const int u = gid + i * kGroupThreads, t = c * 16 + (u >> 4), at = f0 + (u & 15) * 8;
+                            if (sh.token[t].id == kNoRequest || at >= a.features) continue;
+                            const uint4 y = *reinterpret_cast<const uint4*>(stage + (u >> 4) * kProjRows + (u & 15) * 8);
+                            uint16_t* p = reinterpret_cast<uint16_t*>(a.out) + (t0 + t) * a.ldo + at;
+                            if (at + 8 <= a.features) *reinterpret_cast<uint4*>(p) = y;
+                            else {
+                                const uint32_t e[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                            for (int k = 0; k < 8; ++k)
-                                if (at + k < a.features) p[k] = (uint16_t)(e[k >> 1] >> (16 * (k & 1)));
+                                for (int k = 0; k < 8; ++k)
+                                    if (at + k < a.features) p[k] = (uint16_t)(e[k >> 1] >> (16 * (k & 1)));
+                            }
                         }
                     }
-                    // (two buffers in turn: the next barrier tells that this one has been read)
-                    stage = reinterpret_cast<uint16_t*>(ring) + (group * 2 + (stage == reinterpret_cast<uint16_t*>(ring) + group * 2 * 16 * kProjRows)) * 16 * kProjRows;
                 }
-            }
+            };
+            const auto finish_as = [&](auto type) {
+                if (cranks > 1) finish(type, std::integral_constant<int, 0>());
+                else if (wide_out) finish(type, std::integral_constant<int, 1>());
+                else finish(type, std::integral_constant<int, 2>());
+            };
+            if (BACK ? a.out_bf16 != 0 : BF16) finish_as(__nv_bfloat16());
+            else finish_as(__half());
             tc_fence_before();
         }
     }
@@ -660,7 +680,7 @@ int encode_map(zipml_ctx* ctx, CUtensorMapDataType type, const void* base, int64
 template <int NT, bool BACK, bool BF16, bool PAIR = false>
 static int launch_project_as(zipml_ctx* ctx, const ProjectArgs& a, const CUtensorMap& tokens_map, const CUtensorMap& codes_map, int ranks) {
     auto kernel = &project_kernel<NT, BACK, BF16, PAIR>;
-    const size_t smem = 1024 + ProjShape<NT, PAIR>::kRing + sizeof(ProjShared<NT>);
+    const size_t smem = 1024 + ProjShape<NT, PAIR>::kRing + sizeof(ProjShared<NT, PAIR>);
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return cuda_status(e);
     constexpr int kTileRows = PAIR ? 2 * kProjRows : kProjRows;
