@@ -249,18 +249,17 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
     const auto up_stages = [&] { return (sh.entries * rank8 + kRankChunk - 1) / kRankChunk; };      // of the adapters' ranks
 
     if (warp == 0) {
-        // the tokens' operand
-        if (lane == 0) {
-            if (a.early & 2) asm volatile("griddepcontrol.wait;" ::: "memory");
-            int s = 0;
-            RingAt at;
-            RingAt stage, ahead;                                           // stage s, and s - R, whose place it takes
-            for (; s < steps; ++s, at.next(1, R), stage.next(1, L)) {
-                if (s >= R) {
-                    if (!tc_wait(&sh.empty[ahead.slot], ahead.turn, gave_up, a.status, 93)) break;
-                    ahead.next(1, L);
-                }
-                const uint32_t dst = smem_u32(right + at.slot * Shape::kRightBytes);
+        // The tokens' operand.  (Here and below a warp comes to its waits as a whole and one lane, elected, issues: see tc_elect.)
+        if (a.early & 2) asm volatile("griddepcontrol.wait;" ::: "memory");
+        int s = 0;
+        RingAt at, stage, ahead;                                           // stage s, and s - R, whose place it takes
+        for (; s < steps; ++s, at.next(1, R), stage.next(1, L)) {
+            if (s >= R) {
+                if (!__all_sync(0xffffffffu, tc_wait(&sh.empty[ahead.slot], ahead.turn, gave_up, a.status, 93))) break;
+                ahead.next(1, L);
+            }
+            const uint32_t dst = smem_u32(right) + at.slot * Shape::kRightBytes;
+            if (tc_elect()) {
                 if constexpr (PAIR) {
                     // (both halves count on the first CTA's barrier; the other's bytes may come before they are expected)
                     if (side == 0) mbar_arrive_expect_tx(&sh.full[stage.slot], 2 * Shape::kRightBytes);
@@ -270,25 +269,30 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                     tc_copy_2d(dst, &tokens_map, (step0 + s) * kProjDepth, (int)t0, &sh.full[stage.slot]);
                 }
             }
-            if (s < steps)                                                 // (its stages' barriers want the unpacking warps too: they are waited for a while)
-                for (int i = max(0, s - R); i < s; ++i)
-                    if (side == 0) tc_drain(&sh.full[i % L], (i / L) & 1);
+            __syncwarp();
         }
+        if (s < steps && lane == 0)                                        // (its stages' barriers want the unpacking warps too: they are waited for a while)
+            for (int i = max(0, s - R); i < s; ++i)
+                if (side == 0) tc_drain(&sh.full[i % L], (i / L) & 1);
+        __syncwarp();
     } else if (warp == 2) {
         // the packed codes
-        if (lane == 0) {
-            int s = 0;
-            RingAt at;
-            for (; s < steps; ++s, at.next(1, code_slots)) {
-                if (s >= code_slots && !tc_wait(&sh.codes_empty[at.slot], at.turn ^ 1u, gave_up, a.status, 94)) break;
+        int s = 0;
+        RingAt at;
+        for (; s < steps; ++s, at.next(1, code_slots)) {
+            if (s >= code_slots && !__all_sync(0xffffffffu, tc_wait(&sh.codes_empty[at.slot], at.turn ^ 1u, gave_up, a.status, 94))) break;
+            const int depth = (step0 + s) * kProjDepth;
+            const uint32_t dst = smem_u32(packed) + at.slot * code_bytes;
+            if (tc_elect()) {
                 mbar_arrive_expect_tx(&sh.codes_full[at.slot], code_bytes);
-                const int depth = (step0 + s) * kProjDepth;
-                if (BACK) tc_copy_2d(smem_u32(packed + at.slot * code_bytes), &codes_map, depth / 8 * cb, f0, &sh.codes_full[at.slot]);
-                else tc_copy_2d(smem_u32(packed + at.slot * code_bytes), &codes_map, f0 / 8 * cb, depth, &sh.codes_full[at.slot]);
+                if (BACK) tc_copy_2d(dst, &codes_map, depth / 8 * cb, f0, &sh.codes_full[at.slot]);
+                else tc_copy_2d(dst, &codes_map, f0 / 8 * cb, depth, &sh.codes_full[at.slot]);
             }
-            if (s < steps)
-                for (int i = max(0, s - code_slots); i < s; ++i) tc_drain(&sh.codes_full[i % code_slots], (i / code_slots) & 1);
+            __syncwarp();
         }
+        if (s < steps && lane == 0)
+            for (int i = max(0, s - code_slots); i < s; ++i) tc_drain(&sh.codes_full[i % code_slots], (i / code_slots) & 1);
+        __syncwarp();
     } else if (warp == 3) {
         // what the first stage has found out about the tokens, and the adapters they need: each with the window of its tokens
         if (a.early) asm volatile("griddepcontrol.wait;" ::: "memory");
