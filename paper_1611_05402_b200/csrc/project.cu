@@ -181,11 +181,19 @@ __device__ __forceinline__ bool unpack_stage(const uint8_t* codes, uint8_t* oper
     return true;
 }
 
-// A 16-bit pair with what is not finite replaced by zero.
-__device__ __forceinline__ uint32_t finite_pair(uint32_t w, uint32_t exponent, bool& bad) {
-    if ((w & exponent) == exponent) { w &= 0xffff0000u; bad = true; }
-    if ((w & (exponent << 16)) == (exponent << 16)) { w &= 0x0000ffffu; bad = true; }
-    return w;
+// Eight 16-bit values with what is not finite replaced by zero.  `lowest`: the exponent's lowest bit in both halves of a word; added to a value
+// without its sign it carries into the sign's place exactly where the exponent is all ones.
+__device__ __forceinline__ uint32_t not_finite(uint32_t w, uint32_t lowest) { return ((w & 0x7fff7fffu) + lowest) & 0x80008000u; }
+__device__ __forceinline__ void keep_finite(uint4& w, uint32_t lowest, bool& bad) {
+    if ((not_finite(w.x, lowest) | not_finite(w.y, lowest) | not_finite(w.z, lowest) | not_finite(w.w, lowest)) == 0) return;
+    bad = true;
+    uint32_t* p = &w.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t n = not_finite(p[i], lowest);
+        if (n & 0x8000u) p[i] &= 0xffff0000u;
+        if (n & 0x80000000u) p[i] &= 0x0000ffffu;
+    }
 }
 
 template <int NT, bool BACK, bool BF16, bool PAIR>
@@ -465,7 +473,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
         if (ok && rank8 > 0) {
             if (a.early) asm volatile("griddepcontrol.wait;" ::: "memory");
             const bool bf16 = BACK ? a.out_bf16 != 0 : BF16;
-            const uint32_t exponent = bf16 ? 0x7f80u : 0x7c00u;
+            const uint32_t lowest = bf16 ? 0x00800080u : 0x04000400u;
             const uint16_t* up = reinterpret_cast<const uint16_t*>(a.up);
             const bool wide = ((reinterpret_cast<uintptr_t>(up) | (uintptr_t)((int64_t)a.features * 2)) & 15) == 0;
             const bool wide_h = ((reinterpret_cast<uintptr_t>(a.hidden) | (uintptr_t)(a.rank * 4)) & 15) == 0;
@@ -499,13 +507,19 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 }
             };
             const auto load_stage = [&](int j) {
+                // (a thread takes 8 features of every eighth rank: eight neighbouring ranks of the depth are one adapter's)
+                static_assert(kGroupThreads == 8 * 16, "a unit of ranks a turn");
+                const int f = f0 + (gid & 15) * 8, there = min(max(a.features - f, 0), 8);
+                const uint16_t* column = up + f;
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
-                    const int u = gid + i * kGroupThreads, at = j * kRankChunk + (u >> 4), f = f0 + (u & 15) * 8;
-                    const int e = (int)__umulhi((uint32_t)at, per_rank8), r = at - e * rank8;
+                    const int at = j * kRankChunk + i * 8, e = (int)__umulhi((uint32_t)at, per_rank8), r = at - e * rank8 + (gid >> 4);
                     w[i] = make_uint4(0, 0, 0, 0);
-                    if (e < entries && r < a.rank)
-                        w[i] = load8_16(up + ((int64_t)sh.entry_id[e] * a.rank + r) * a.features + f, min(max(a.features - f, 0), 8), wide);
+                    if (e < entries && r < a.rank) {
+                        const uint16_t* p = column + ((int64_t)sh.entry_id[e] * a.rank + r) * a.features;
+                        if (wide && there == 8) w[i] = *reinterpret_cast<const uint4*>(p);
+                        else w[i] = load8_16(p, there, false);
+                    }
                 }
                 lo = PAIR ? side * Shape::kRightRows : sh.window_lo[j];
                 const int n = PAIR ? Shape::kRightRows : sh.window_n[j];
@@ -525,8 +539,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 for (int i = 0; i < U; ++i) {
                     const int u = gid + i * kGroupThreads, k = u >> 4, chunk = u & 15;
                     if (k >= padded) continue;
-                    w[i].x = finite_pair(w[i].x, exponent, bad); w[i].y = finite_pair(w[i].y, exponent, bad);
-                    w[i].z = finite_pair(w[i].z, exponent, bad); w[i].w = finite_pair(w[i].w, exponent, bad);
+                    keep_finite(w[i], lowest, bad);
                     *reinterpret_cast<uint4*>(dst + (chunk >> 3) * (kLeftBytes / 2) + k * 128 + (((chunk & 7) ^ (k & 7)) << 4)) = w[i];
                 }
                 uint8_t* tok = right + group * Shape::kRightBytes;
