@@ -144,13 +144,15 @@ def _ptr(t, dtype=None, device=None):
     return C.c_void_p(t.data_ptr())
 
 
-def _rows(t, device, dtypes=DTYPES):
-    """(pointer, dtype, rows, columns, leading dimension) of a matrix whose rows are contiguous."""
-    assert t.dim() == 2 and t.dtype in dtypes, f"expected a matrix of one of {sorted(map(str, dtypes))}, got {tuple(t.shape)} of {t.dtype}"
+def _rows(t, device):
+    """(address, dtype, rows, columns, leading dimension) of a matrix whose rows are contiguous."""
+    rows, columns = t.shape
+    ld, unit = t.stride()
+    dtype = DTYPES.get(t.dtype)
+    assert dtype is not None, f"expected one of {sorted(map(str, DTYPES))}, got {t.dtype}"
     assert t.device == device, f"expected a tensor on {device}, got {t.device}"
-    assert t.shape[1] <= 1 or t.stride(1) == 1, "rows must be contiguous"
-    ld = t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
-    return C.c_void_p(t.data_ptr()), DTYPES[t.dtype], t.shape[0], t.shape[1], ld
+    assert unit == 1 or columns <= 1, "rows must be contiguous"
+    return t.data_ptr(), dtype, rows, columns, ld if rows > 1 and ld > columns else columns
 
 
 class Checkpoint:
@@ -162,11 +164,7 @@ class Checkpoint:
         self.codes, self.grids, self.m, self.n, self.group, self.row_bytes = codes, grids, m, n, group, codes.shape[1]
 
     def c_struct(self):
-        d = CCheckpoint()
-        d.struct_size = C.sizeof(CCheckpoint)
-        d.group, d.m, d.n, d.row_bytes = self.group, self.m, self.n, self.row_bytes
-        d.codes, d.grids = self.codes.data_ptr(), self.grids.data_ptr()
-        return d
+        return CCheckpoint(C.sizeof(CCheckpoint), self.group, self.m, self.n, self.row_bytes, self.codes.data_ptr(), self.grids.data_ptr())
 
     @property
     def packed_bytes(self):
@@ -184,14 +182,12 @@ class Adapters:
 
     def c_struct(self, starts, which):
         """With the requests that use them: starts (requests + 1,) and which (requests,), int32 on the device."""
+        requests = which.numel()
         assert starts.dtype == which.dtype == torch.int32 and starts.is_contiguous() and which.is_contiguous()
-        assert starts.device == which.device == self.a.device and starts.numel() == which.numel() + 1
-        d = CAdapters()
-        d.struct_size = C.sizeof(CAdapters)
-        d.dtype, d.count, d.rank, d.requests = DTYPES.get(self.a.dtype, -1), self.a.shape[0], self.a.shape[1], which.numel()
-        d.a, d.b, d.starts, d.which = self.a.data_ptr(), self.b.data_ptr(), starts.data_ptr(), which.data_ptr()
-        d.scale = self.scale.data_ptr() if self.scale is not None else None
-        return d
+        assert starts.device == which.device == self.a.device and starts.numel() == requests + 1
+        count, rank, _ = self.a.shape
+        return CAdapters(C.sizeof(CAdapters), DTYPES.get(self.a.dtype, -1), count, rank, self.a.data_ptr(), self.b.data_ptr(),
+                         None if self.scale is None else self.scale.data_ptr(), requests, 0, starts.data_ptr(), which.data_ptr())
 
 
 class Dataset:
@@ -205,15 +201,10 @@ class Dataset:
         self.feat_lo, self.feat_step, self.levels = feat_lo, feat_step, levels
 
     def c_struct(self):
-        d = CDataset()
-        d.struct_size = C.sizeof(CDataset)
-        d.bits, d.level_mode, d.m, d.n, d.row_bytes = self.bits, self.level_mode, self.m, self.n, self.row_bytes
-        d.layout = self.layout
-        d.plane1, d.plane2 = self.plane1.data_ptr(), self.plane2.data_ptr()
-        d.feat_lo = self.feat_lo.data_ptr() if self.feat_lo is not None else None
-        d.feat_step = self.feat_step.data_ptr() if self.feat_step is not None else None
-        d.levels = self.levels.data_ptr() if self.levels is not None else None
-        return d
+        lo, step, levels = self.feat_lo, self.feat_step, self.levels
+        return CDataset(C.sizeof(CDataset), self.bits, self.level_mode, self.layout, self.m, self.n, self.row_bytes, self.plane1.data_ptr(),
+                        self.plane2.data_ptr(), None if lo is None else lo.data_ptr(), None if step is None else step.data_ptr(),
+                        None if levels is None else levels.data_ptr())
 
     @property
     def packed_bytes(self):
@@ -503,8 +494,7 @@ class Context:
         """X (m, n) fp32, bf16 or fp16 -> Checkpoint (or into `out`, one of the same shape and group)."""
         ptr, dtype, m, n, ld = _rows(X, self.device)
         if out is None:
-            out = Checkpoint(torch.empty((m, (n + 15) // 16 * 16), dtype=torch.uint8, device=self.device),
-                             torch.empty((m, -(-n // group), 2), dtype=torch.float32, device=self.device), m, n, group)
+            out = Checkpoint(X.new_empty((m, (n + 15) // 16 * 16), dtype=torch.uint8), X.new_empty((m, -(-n // group), 2), dtype=torch.float32), m, n, group)
         assert out.codes.device == self.device
         d = out.c_struct()
         _check(lib().zipml_checkpoint_encode(self._h, ptr, dtype, m, n, ld, seed, C.byref(d)), "zipml_checkpoint_encode")
@@ -512,7 +502,7 @@ class Context:
 
     def zipml_checkpoint_decode(self, data, dtype=torch.bfloat16, out=None):
         """The checkpoint's values as (m, n) of `dtype` (or into `out`, of its own type)."""
-        out = torch.empty((data.m, data.n), dtype=dtype, device=self.device) if out is None else out
+        out = data.codes.new_empty((data.m, data.n), dtype=dtype) if out is None else out
         ptr, kind, m, n, ld = _rows(out, self.device)
         assert (m, n) == (data.m, data.n) and data.codes.device == self.device
         d = data.c_struct()
@@ -532,7 +522,7 @@ class Context:
         outside the requests are left as they were (uninitialised in a new result)."""
         ptr, dtype, tokens, n_in, ld = _rows(X, self.device)
         assert n_in == weights.m
-        out = torch.empty((tokens, weights.n), dtype=X.dtype, device=self.device) if out is None else out
+        out = X.new_empty((tokens, weights.n)) if out is None else out
         optr, odtype, orows, ocols, old = _rows(out, self.device)
         assert (orows, ocols, odtype) == (tokens, weights.n, dtype)
         a = self._adapters(weights, adapters, starts, which)
@@ -550,25 +540,27 @@ class Context:
         assert n_out == weights.n
         optr, old = None, 0
         if want_input:
-            out = torch.empty((tokens, weights.m), dtype=dY.dtype, device=self.device) if out is None else out
+            out = dY.new_empty((tokens, weights.m)) if out is None else out
             optr, odtype, orows, ocols, old = _rows(out, self.device)
             assert (orows, ocols, odtype) == (tokens, weights.m, dtype)
         else:
             out = None
         a = self._adapters(weights, adapters, starts, which)
-        if adapters is not None and checkpoint is not None and grad_a is None:
-            grad_a = torch.empty(adapters.a.shape, dtype=torch.float32, device=self.device)
-        if adapters is not None and hidden is not None and grad_b is None:
-            grad_b = torch.empty(adapters.b.shape, dtype=torch.float32, device=self.device)
-        assert hidden is None or (adapters is not None and hidden.shape == (tokens, adapters.a.shape[1]))
-        assert grad_a is None or (adapters is not None and grad_a.shape == adapters.a.shape)
-        assert grad_b is None or (adapters is not None and grad_b.shape == adapters.b.shape)
+        if adapters is None:
+            assert hidden is None and grad_a is None and grad_b is None
+        else:
+            ashape, bshape = adapters.a.shape, adapters.b.shape
+            if checkpoint is not None and grad_a is None:
+                grad_a = dY.new_empty(ashape, dtype=torch.float32)
+            if hidden is not None and grad_b is None:
+                grad_b = dY.new_empty(bshape, dtype=torch.float32)
+            assert hidden is None or hidden.shape == (tokens, ashape[1])
+            assert (grad_a is None or grad_a.shape == ashape) and (grad_b is None or grad_b.shape == bshape)
         assert checkpoint is None or checkpoint.codes.device == self.device
-        w, c = weights.c_struct(), None if checkpoint is None else checkpoint.c_struct()
-        f32 = torch.float32
-        _check(lib().zipml_project_backward(self._h, C.byref(w), None if a is None else C.byref(a), ptr, dtype, tokens, ld, _ptr(hidden, f32, self.device),
-                                            None if c is None else C.byref(c), optr, old, _ptr(grad_a, f32, self.device),
-                                            _ptr(grad_b, f32, self.device)), "zipml_project_backward")
+        w, c, f32, device = weights.c_struct(), None if checkpoint is None else checkpoint.c_struct(), torch.float32, self.device
+        _check(lib().zipml_project_backward(self._h, C.byref(w), None if a is None else C.byref(a), ptr, dtype, tokens, ld, _ptr(hidden, f32, device),
+                                            None if c is None else C.byref(c), optr, old, _ptr(grad_a, f32, device), _ptr(grad_b, f32, device)),
+               "zipml_project_backward")
         return out, grad_a, grad_b
 
     def zipml_train_host(self, A_host, b_host, x_host, bits, batch, lr, epochs, optimal_levels=False, hist_bins=1024,

@@ -38,6 +38,16 @@ bool capturing(zipml_ctx* ctx) {
     return capture != cudaStreamCaptureStatusNone;
 }
 
+int allow_shared(zipml_ctx* ctx, const void* kernel, size_t bytes) {
+    const int at = (int)(((reinterpret_cast<uintptr_t>(kernel) >> 4) * 0x9E3779B97F4A7C15ull) >> 58);
+    if (bytes > kMostShared) return ZIPML_ERR_WORKSPACE;
+    if (ctx->allowed[at] == kernel) return ZIPML_OK;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostShared);
+    if (e != cudaSuccess) return cuda_status(e);
+    ctx->allowed[at] = kernel;
+    return ZIPML_OK;
+}
+
 int project_reserve(zipml_ctx* ctx, size_t bytes, unsigned char** block) {
     if (bytes > ctx->project_bytes || ctx->project_blocks == 0) {
         if (capturing(ctx) || ctx->project_blocks == zipml_ctx::kProjectBlocks) return ZIPML_ERR_WORKSPACE;

@@ -40,6 +40,7 @@ struct zipml_ctx {
     unsigned char* project_ws[kProjectBlocks] = {};
     int project_blocks = 0;
     size_t project_bytes = 0;
+    const void* allowed[64] = {};   // kernels that have been allowed their shared memory (see allow_shared), by hash, the newest wins
 };
 
 namespace zipml {
@@ -52,6 +53,10 @@ int cuda_status(cudaError_t e);                       // ZIPML_OK or ZIPML_ERR_C
 int ws_reserve(zipml_ctx* ctx, size_t bytes);         // grow ctx->ws to at least `bytes`
 int stage_reserve(zipml_ctx* ctx, size_t bytes);
 int project_reserve(zipml_ctx* ctx, size_t bytes, unsigned char** block);   // ZIPML_ERR_WORKSPACE where it would have to grow during capture
+// Lets a kernel have up to kMostShared bytes of dynamic shared memory: asked for once a context and kernel, and always that much, so that
+// contexts cannot take it from each other.
+constexpr size_t kMostShared = 224 * 1024;      // (beside a kernel's fixed shared memory)
+int allow_shared(zipml_ctx* ctx, const void* kernel, size_t bytes);
 bool capturing(zipml_ctx* ctx);                       // the context's stream is being recorded into a graph
 // `bytes` of exchange words between clusters, and the tag of the first of `steps` steps.  At most two buffers in turn, 8 clusters, 16
 // bytes for each of 8,192 features and what the last slice or column has past them.

@@ -698,8 +698,9 @@ template <int NT, bool BACK, bool BF16, bool PAIR = false>
 static int launch_project_as(zipml_ctx* ctx, const ProjectArgs& a, const CUtensorMap& tokens_map, const CUtensorMap& codes_map, int ranks) {
     auto kernel = &project_kernel<NT, BACK, BF16, PAIR>;
     const size_t smem = 1024 + ProjShape<NT, PAIR>::kRing + sizeof(ProjShared<NT, PAIR>);
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return cuda_status(e);
+    static_assert(1024 + ProjShape<NT, PAIR>::kRing + sizeof(ProjShared<NT, PAIR>) <= kMostShared, "what a block may have");
+    const int rc = allow_shared(ctx, reinterpret_cast<const void*>(kernel), smem);
+    if (rc != ZIPML_OK) return rc;
     constexpr int kTileRows = PAIR ? 2 * kProjRows : kProjRows;
     if (PAIR) ranks = 2;
     const int64_t tiles = (a.tokens + NT - 1) / NT * ((a.features + kTileRows - 1) / kTileRows);
@@ -716,7 +717,7 @@ static int launch_project_as(zipml_ctx* ctx, const ProjectArgs& a, const CUtenso
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = a.early ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, kernel, a, tokens_map, codes_map);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a, tokens_map, codes_map);
     ctx->launches += 1;
     return cuda_status(e != cudaSuccess ? e : cudaGetLastError());
 }

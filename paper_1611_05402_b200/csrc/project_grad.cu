@@ -321,8 +321,8 @@ template <int MT>
 static int launch_grad_as(zipml_ctx* ctx, const GradArgs& a, const CUtensorMap& codes_map, const CUtensorMap& dy_map) {
     const int blocks = a.down_blocks + a.up_blocks, passes = (a.rank + MT * 16 - 1) / (MT * 16);
     const size_t smem = 1024 + kGradWarps * grad_slots(MT) * kGradSlotBytes + sizeof(GradShared);
-    cudaError_t e = cudaFuncSetAttribute(&grad_kernel<MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return cuda_status(e);
+    const int rc = allow_shared(ctx, reinterpret_cast<const void*>(&grad_kernel<MT>), smem);
+    if (rc != ZIPML_OK) return rc;
     int ranks = 1;
     while (ranks < 8 && (int64_t)blocks * a.adapters * passes * ranks < 2 * ctx->sm_count && (int64_t)ranks * kGradWarps * kGradChunk < a.tokens) ranks *= 2;
     if (a.adapters > 65535 || (int64_t)blocks * ranks > 0x7fffffffLL) return ZIPML_ERR_WORKSPACE;
@@ -336,7 +336,7 @@ static int launch_grad_as(zipml_ctx* ctx, const GradArgs& a, const CUtensorMap& 
     attr[0].val.clusterDim.x = (unsigned)ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, &grad_kernel<MT>, a, codes_map, dy_map);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, &grad_kernel<MT>, a, codes_map, dy_map);
     ctx->launches += 1;
     return cuda_status(e != cudaSuccess ? e : cudaGetLastError());
 }

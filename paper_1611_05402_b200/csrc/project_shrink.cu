@@ -579,8 +579,8 @@ static int launch_tall(zipml_ctx* ctx, const ShrinkArgs& a, int dtype, bool sums
         rc = encode_map(ctx, type, a.down, a.columns, (int64_t)a.adapters * a.rank, (int64_t)a.columns * 2, kTallDepth, f.ranks8, CU_TENSOR_MAP_SWIZZLE_128B, &down_map);
     if (rc != ZIPML_OK) return rc;
     auto kernel = dtype == ZIPML_BF16 ? &shrink_tall_kernel<true> : &shrink_tall_kernel<false>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return cuda_status(e);
+    rc = allow_shared(ctx, reinterpret_cast<const void*>(kernel), smem);
+    if (rc != ZIPML_OK) return rc;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(tiles * ranks));
     cfg.blockDim = dim3(kTallThreads);
@@ -591,7 +591,7 @@ static int launch_tall(zipml_ctx* ctx, const ShrinkArgs& a, int dtype, bool sums
     attr[0].val.clusterDim.x = (unsigned)ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kernel, a, f, z_map, down_map);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a, f, z_map, down_map);
     ctx->launches += 1;
     return cuda_status(e != cudaSuccess ? e : cudaGetLastError());
 }
@@ -609,8 +609,8 @@ static int launch_shrink_as(zipml_ctx* ctx, const ShrinkArgs& a) {
     const size_t smem = (size_t)kShrinkWarps * kShrinkRows * RT * 8 * sizeof(float);
     auto kernel = &shrink_kernel<T, BACK, RT>;
     if (smem > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return cuda_status(e);
+        const int rc = allow_shared(ctx, reinterpret_cast<const void*>(kernel), smem);
+        if (rc != ZIPML_OK) return rc;
     }
     const int64_t tiles = (a.tokens + kShrinkRows - 1) / kShrinkRows;
     // Few tiles: the columns over the CTAs of a cluster, the tile's adapters over several clusters, until the GPU is about full.
