@@ -149,36 +149,38 @@ __device__ __forceinline__ uint4 centred_chunk(uint32_t w0, uint32_t w1) {      
                       centred_pair<BF16, CB>(__byte_perm(w1, kTop, 0x4140)), centred_pair<BF16, CB>(__byte_perm(w1, kTop, 0x4342)));
 }
 
-// One stage's codes into the left operand, four units of 16 codes a thread.  Bank conflicts: eight lanes store 16 bytes each at a time;
-// forward they hold one depth's 8 units, whose first halves would meet in pairs 8 KB apart, so the upper 64 features store their second
-// half first.  The codes' slot is given back as soon as they are in registers; false where the left operand's wait gave up.
-template <bool BF16, int CB, bool BACK, class Free, class Wait>
-__device__ __forceinline__ bool unpack_stage(const uint8_t* codes, uint8_t* operand, int gid, Free free, Wait wait) {
-    constexpr int U = kProjRows * kProjDepth / 16 / kGroupThreads;
-    uint32_t w[U][4];
-#pragma unroll
-    for (int i = 0; i < U; ++i) load_codes<CB>(codes + (gid + i * kGroupThreads) * 2 * CB, w[i]);
-    free();
-    if (!wait()) return false;
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const int u = gid + i * kGroupThreads;
-        codes_to_bytes<CB>(w[i]);
-        const uint4 first = centred_chunk<BF16, CB>(w[i][0], w[i][1]), second = centred_chunk<BF16, CB>(w[i][2], w[i][3]);
+// A thread's place in a stage: kUnits units of 16 codes, from one to the next the same distance on in the packed codes and in the left
+// operand.  Bank conflicts: eight lanes store 16 bytes each at a time, so four take one 128-byte row of the operand and four the next,
+// whose swizzles differ in the lowest bit.  Forward: a unit is 16 features of one depth (MN-major, 64 features a row); backward 16 of
+// the depth of one feature.
+constexpr int kUnits = kProjRows * kProjDepth / 16 / kGroupThreads;
+template <bool BACK>
+struct UnitPlace {
+    uint32_t from, to;                        // unit of the packed codes, byte of the operand
+    static constexpr uint32_t kFromStep = kGroupThreads, kToStep = BACK ? 32 * 128 : 16 * 128;
+    __device__ __forceinline__ explicit UnitPlace(int gid) {
         if constexpr (BACK) {
-            const int row = u >> 2, chunk = 2 * (u & 3);                        // 16 of the depth of one feature
-            uint8_t* p = operand + row * 128;
-            *reinterpret_cast<uint4*>(p + ((chunk ^ (row & 7)) << 4)) = first;
-            *reinterpret_cast<uint4*>(p + (((chunk + 1) ^ (row & 7)) << 4)) = second;
+            const uint32_t row = gid >> 2, chunk = 2 * (gid & 3);
+            from = gid;
+            to = row * 128 + ((chunk ^ (row & 7)) << 4);
         } else {
-            const int k = u >> 3, f16 = u & 7, chunk = 2 * (f16 & 3);           // 16 features of one depth
-            uint8_t* p = operand + (f16 >> 2) * (kLeftBytes / 2) + k * 128;
-            const bool swap = f16 >= 4;
-            *reinterpret_cast<uint4*>(p + (((chunk + swap) ^ (k & 7)) << 4)) = swap ? second : first;
-            *reinterpret_cast<uint4*>(p + (((chunk + !swap) ^ (k & 7)) << 4)) = swap ? first : second;
+            const uint32_t k = (gid >> 4) * 2 + (gid >> 2 & 1), f16 = (gid & 3) + (gid >> 3 & 1) * 4, chunk = 2 * (f16 & 3);
+            from = k * 8 + f16;
+            to = (f16 >> 2) * (kLeftBytes / 2) + k * 128 + ((chunk ^ (k & 7)) << 4);
         }
     }
-    return true;
+};
+static_assert(kGroupThreads == 128, "a turn of units is 16 depths of 128 features, or 32 features of 64 depths");
+
+template <bool BF16, int CB, bool BACK>
+__device__ __forceinline__ void unpack_stage(uint32_t (&w)[kUnits][4], uint8_t* to) {
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        codes_to_bytes<CB>(w[i]);
+        uint8_t* p = to + i * UnitPlace<BACK>::kToStep;
+        *reinterpret_cast<uint4*>(p) = centred_chunk<BF16, CB>(w[i][0], w[i][1]);
+        *reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(p) ^ 16) = centred_chunk<BF16, CB>(w[i][2], w[i][3]);
+    }
 }
 
 // Eight 16-bit values with what is not finite replaced by zero.  `lowest`: the exponent's lowest bit in both halves of a word; added to a value
@@ -448,27 +450,47 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             alpha = a.step[feature];
             beta = fmaf(a.center, alpha, a.lo[feature]);
         }
-        int s = group;
-        bool ok = true;
-        RingAt ca, la;
-        ca.next(group, code_slots); la.next(group, L);
-        for (; s < steps; s += kGroups, ca.next(kGroups, code_slots), la.next(kGroups, L)) {
-            ok = __all_sync(0xffffffffu, tc_wait(&sh.codes_full[ca.slot], ca.turn, gave_up, a.status, 99));       // (a warp gives up as a whole)
-            if (!ok) break;
-            const uint8_t* src = packed + ca.slot * code_bytes;
-            uint8_t* dst = left + la.slot * kLeftBytes;
-            const auto free = [&] {
+        // (a warp gives up as a whole; the next stage's codes are on their way into registers while this one's are unpacked)
+        const auto unpack = [&](auto bits) {
+            constexpr int CB = decltype(bits)::value;
+            const UnitPlace<BACK> place(gid);
+            RingAt ca, la;
+            ca.next(group, code_slots);
+            la.next(group, L);
+            uint32_t w[kUnits][4], next[kUnits][4];
+            const auto fetch = [&](uint32_t (&v)[kUnits][4]) {
+                if (!__all_sync(0xffffffffu, tc_wait(&sh.codes_full[ca.slot], ca.turn, gave_up, a.status, 99))) return false;
+                const uint8_t* p = packed + ca.slot * code_bytes + place.from * (2 * CB);
+#pragma unroll
+                for (int i = 0; i < kUnits; ++i) load_codes<CB>(p + i * UnitPlace<BACK>::kFromStep * (2 * CB), v[i]);
+                return true;
+            };
+            const auto give_back = [&] {
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.codes_empty[ca.slot]);
+                ca.next(kGroups, code_slots);
             };
-            const auto wait = [&] { return s < L || __all_sync(0xffffffffu, tc_wait(&sh.empty[la.slot], la.turn ^ 1u, gave_up, a.status, 100)); };
-            if (cb == 8) ok = unpack_stage<BF16, 8, BACK>(src, dst, gid, free, wait);
-            else if (cb == 4) ok = unpack_stage<BF16, 4, BACK>(src, dst, gid, free, wait);
-            else ok = unpack_stage<BF16, 2, BACK>(src, dst, gid, free, wait);
-            if (!ok) break;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.written[la.slot]);
-        }
+            if (group >= steps) return true;
+            if (!fetch(w)) return false;
+            give_back();
+            for (int s = group; s < steps; s += kGroups, la.next(kGroups, L)) {
+                const bool more = s + kGroups < steps;
+                if (more && !fetch(next)) return false;
+                if (s >= L && !__all_sync(0xffffffffu, tc_wait(&sh.empty[la.slot], la.turn ^ 1u, gave_up, a.status, 100))) return false;
+                unpack_stage<BF16, CB, BACK>(w, left + la.slot * kLeftBytes + place.to);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.written[la.slot]);
+                if (more) {
+                    give_back();
+#pragma unroll
+                    for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) w[i][k] = next[i][k];
+                }
+            }
+            return true;
+        };
+        bool ok = cb == 8 ? unpack(std::integral_constant<int, 8>()) : cb == 4 ? unpack(std::integral_constant<int, 4>()) : unpack(std::integral_constant<int, 2>());
         if (ok) ok = __all_sync(0xffffffffu, tc_wait(&sh.plan, 0, gave_up, a.status, 101));
         if (ok && rank8 > 0) {
             if (a.early) asm volatile("griddepcontrol.wait;" ::: "memory");
