@@ -124,17 +124,18 @@ __device__ __forceinline__ void codes_to_bytes(uint32_t (&w)[4]) {
 }
 
 // Two codes, in the low bytes of p's halves under the byte of 128 (bf16) or 1024 (fp16), as code - 2^(CB-1): the code is the mantissa's
-// lowest bits, and one exact subtraction takes the offset away.  (bf16's mantissa has 7 bits: an 8-bit code's top bit would count as
-// exponent, so it chooses between 128 and 256 on the other side.)
+// lowest bits, and one exact subtraction takes the offset away.  bf16's mantissa has 7 bits: an 8-bit code's top bit counts as exponent there,
+// and the value is 128 + code below 128, 256 + 2 (code - 128) from there on; less 256 it is what it should be, or twice that.  (Byte and
+// logic instructions run at half the rate of the 16-bit arithmetic's and bound the unpacking: two of each a pair.)
 template <bool BF16, int CB>
 __device__ __forceinline__ uint32_t centred_pair(uint32_t p) {
     if constexpr (BF16) {
-        uint32_t a = p, b = CB == 4 ? 0x43084308u : 0x43024302u;
+        const uint32_t b = CB == 8 ? 0x43804380u : CB == 4 ? 0x43084308u : 0x43024302u;
+        __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&p), *reinterpret_cast<const __nv_bfloat162*>(&b));
         if constexpr (CB == 8) {
-            a = p & 0xff7fff7fu;
-            b = (p & 0x00800080u) ^ 0x43804380u;
+            const uint32_t half = (p & 0x00800080u) ^ 0x3F803F80u;           // a half where the top bit is set, else one
+            v = __hmul2(v, *reinterpret_cast<const __nv_bfloat162*>(&half));
         }
-        const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
         return *reinterpret_cast<const uint32_t*>(&v);
     } else {
         const uint32_t b = CB == 8 ? 0x64806480u : CB == 4 ? 0x64086408u : 0x64026402u;
