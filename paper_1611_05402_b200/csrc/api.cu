@@ -158,7 +158,7 @@ static int check_projection(const zipml_dataset* w, const zipml_adapters* a, int
     return ZIPML_OK;
 }
 
-static float code_center(int bits) { return (float)(1 << (container_bits(bits) - 1)); }
+static float code_center(int bits) { return (float)(1 << (bits - 1)); }      // (the codes' own middle: what is rounded beside them grows with their distance from it)
 
 }  // namespace zipml
 
@@ -788,7 +788,7 @@ int zipml_project(zipml_ctx* ctx, const zipml_dataset* weights, const zipml_adap
     rc = launch_shrink(ctx, s, dtype, false);
     if (rc != ZIPML_OK) return rc;
     ProjectArgs p{};
-    p.tokens = tokens; p.features = (int)weights->n; p.depth = (int)weights->m; p.bits = container_bits(weights->bits);
+    p.tokens = tokens; p.features = (int)weights->n; p.depth = (int)weights->m; p.bits = weights->bits;
     p.lo = weights->feat_lo; p.step = weights->feat_step; p.center = code_center(weights->bits);
     p.ids = s.ids; p.sum = s.sum; p.hidden_scale = s.hidden_scale; p.hidden = s.hidden;
     p.up = adapters ? adapters->b : nullptr; p.rank = rank; p.requests = s.requests;
@@ -842,7 +842,7 @@ int zipml_project_backward(zipml_ctx* ctx, const zipml_dataset* weights, const z
         if (rc != ZIPML_OK) return rc;
         if (dX) {
             ProjectArgs p{};
-            p.tokens = tokens; p.features = (int)weights->m; p.depth = (int)weights->n; p.bits = container_bits(weights->bits);
+            p.tokens = tokens; p.features = (int)weights->m; p.depth = (int)weights->n; p.bits = weights->bits;
             p.center = s.center;
             p.ids = s.ids; p.sum = s.sum; p.row_scale = s.row_scale; p.hidden_scale = s.hidden_scale; p.hidden = v;
             p.up = adapters ? adapters->a : nullptr; p.rank = rank; p.requests = s.requests;

@@ -14,7 +14,7 @@ namespace cg = cooperative_groups;
 // ---------------------------------------------------------------------------------------------
 // A CTA makes 128 features x NT tokens.  The features stand on the product's 128 rows and the tokens on its columns, so one
 // kernel serves from a token (16 columns, the codes' bytes are what counts) to thousands.  Per 64 of the depth:
-//   codes     a tensor copy brings the packed codes; groups of four warps, each with a stage of its own, turn them into 16-bit whole numbers code - 2^(cb-1), which are exact, and
+//   codes     a tensor copy brings the packed codes; groups of four warps, each with a stage of its own, turn them into 16-bit whole numbers code - 2^(bits-1), which are exact, and
 //             lay them out as the product's left operand.  Forward: a code row is one depth and holds the features (MN-major
 //             operand); backward: a code row is a feature (K-major).
 //   tokens    a tensor copy lays the right operand out itself.
@@ -123,31 +123,36 @@ __device__ __forceinline__ void codes_to_bytes(uint32_t (&w)[4]) {
     }
 }
 
-// Two codes, in the low bytes of p's halves under the byte of 128 (bf16) or 1024 (fp16), as code - 2^(CB-1): the code is the mantissa's
-// lowest bits, and one exact subtraction takes the offset away.  bf16's mantissa has 7 bits: an 8-bit code's top bit counts as exponent there,
-// and the value is 128 + code below 128, 256 + 2 (code - 128) from there on; less 256 it is what it should be, or twice that.  (Byte and
-// logic instructions run at half the rate of the 16-bit arithmetic's and bound the unpacking: two of each a pair.)
-template <bool BF16, int CB>
-__device__ __forceinline__ uint32_t centred_pair(uint32_t p) {
+// Two codes, in the low bytes of p's halves under the byte of 128 (bf16) or 1024 (fp16), as code - center: the code is the mantissa's
+// lowest bits, and one exact subtraction of `base` = that and the center takes the offset away.  EIGHT: 8-bit codes in bf16, whose mantissa has 7
+// bits: a code's top bit counts as exponent there, and the value is 128 + code below 128, 256 + 2 (code - 128) from there on; less 256
+// it is what it should be, or twice that.  (Byte and logic instructions run at half the rate of the 16-bit arithmetic's and bound the
+// unpacking: two of each a pair.)
+template <bool BF16, bool EIGHT>
+__device__ __forceinline__ uint32_t centred_pair(uint32_t p, uint32_t base) {
     if constexpr (BF16) {
-        const uint32_t b = CB == 8 ? 0x43804380u : CB == 4 ? 0x43084308u : 0x43024302u;
-        __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&p), *reinterpret_cast<const __nv_bfloat162*>(&b));
-        if constexpr (CB == 8) {
+        __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&p), *reinterpret_cast<const __nv_bfloat162*>(&base));
+        if constexpr (EIGHT) {
             const uint32_t half = (p & 0x00800080u) ^ 0x3F803F80u;           // a half where the top bit is set, else one
             v = __hmul2(v, *reinterpret_cast<const __nv_bfloat162*>(&half));
         }
         return *reinterpret_cast<const uint32_t*>(&v);
     } else {
-        const uint32_t b = CB == 8 ? 0x64806480u : CB == 4 ? 0x64086408u : 0x64026402u;
-        const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&p), *reinterpret_cast<const __half2*>(&b));
+        const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&p), *reinterpret_cast<const __half2*>(&base));
         return *reinterpret_cast<const uint32_t*>(&v);
     }
 }
-template <bool BF16, int CB>
-__device__ __forceinline__ uint4 centred_chunk(uint32_t w0, uint32_t w1) {      // 8 codes
+template <bool BF16, bool EIGHT>
+__device__ __forceinline__ uint4 centred_chunk(uint32_t w0, uint32_t w1, uint32_t base) {      // 8 codes
     constexpr uint32_t kTop = BF16 ? 0x43434343u : 0x64646464u;
-    return make_uint4(centred_pair<BF16, CB>(__byte_perm(w0, kTop, 0x4140)), centred_pair<BF16, CB>(__byte_perm(w0, kTop, 0x4342)),
-                      centred_pair<BF16, CB>(__byte_perm(w1, kTop, 0x4140)), centred_pair<BF16, CB>(__byte_perm(w1, kTop, 0x4342)));
+    return make_uint4(centred_pair<BF16, EIGHT>(__byte_perm(w0, kTop, 0x4140), base), centred_pair<BF16, EIGHT>(__byte_perm(w0, kTop, 0x4342), base),
+                      centred_pair<BF16, EIGHT>(__byte_perm(w1, kTop, 0x4140), base), centred_pair<BF16, EIGHT>(__byte_perm(w1, kTop, 0x4342), base));
+}
+// The base for codes of so many bits, in both halves: 128 (256 for EIGHT) or 1024, and the center 2^(bits - 1).
+template <bool BF16>
+__device__ __forceinline__ uint32_t centre_base(int bits) {
+    const uint32_t center = 1u << (bits - 1), h = BF16 ? 0x4300u + center : 0x6400u + center;      // (8 bits in bf16: 0x4380, which is 256)
+    return h | h << 16;
 }
 
 // A thread's place in a stage: kUnits units of 16 codes, from one to the next the same distance on in the packed codes and in the left
@@ -173,14 +178,14 @@ struct UnitPlace {
 };
 static_assert(kGroupThreads == 128, "a turn of units is 16 depths of 128 features, or 32 features of 64 depths");
 
-template <bool BF16, int CB, bool BACK>
-__device__ __forceinline__ void unpack_stage(uint32_t (&w)[kUnits][4], uint8_t* to) {
+template <bool BF16, int CB, bool EIGHT, bool BACK>
+__device__ __forceinline__ void unpack_stage(uint32_t (&w)[kUnits][4], uint8_t* to, uint32_t base) {
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
         codes_to_bytes<CB>(w[i]);
         uint8_t* p = to + i * UnitPlace<BACK>::kToStep;
-        *reinterpret_cast<uint4*>(p) = centred_chunk<BF16, CB>(w[i][0], w[i][1]);
-        *reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(p) ^ 16) = centred_chunk<BF16, CB>(w[i][2], w[i][3]);
+        *reinterpret_cast<uint4*>(p) = centred_chunk<BF16, EIGHT>(w[i][0], w[i][1], base);
+        *reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(p) ^ 16) = centred_chunk<BF16, EIGHT>(w[i][2], w[i][3], base);
     }
 }
 
@@ -222,7 +227,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
     const int64_t t0 = (int64_t)(tile / feature_tiles) * NT;
     const int all_steps = (a.depth + kProjDepth - 1) / kProjDepth, per = (all_steps + cranks - 1) / cranks;
     const int step0 = min(crank * per, all_steps), steps = min(per, all_steps - step0);
-    const int cb = a.bits;
+    const int cb = container_bits(a.bits);
     const uint32_t code_bytes = (uint32_t)(kProjRows * kProjDepth / 8 * cb);
     const int code_slots = min(kMostSlots, (int)(Shape::kCodeRing / code_bytes) / kGroups * kGroups);
     volatile int* gave_up = &sh.gave_up;
@@ -452,8 +457,10 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             beta = fmaf(a.center, alpha, a.lo[feature]);
         }
         // (a warp gives up as a whole; the next stage's codes are on their way into registers while this one's are unpacked)
-        const auto unpack = [&](auto bits) {
-            constexpr int CB = decltype(bits)::value;
+        const auto unpack = [&](auto container, auto eight) {
+            constexpr int CB = decltype(container)::value;
+            constexpr bool EIGHT = decltype(eight)::value;
+            const uint32_t base = centre_base<BF16>(a.bits);
             const UnitPlace<BACK> place(gid);
             RingAt ca, la;
             ca.next(group, code_slots);
@@ -478,7 +485,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 const bool more = s + kGroups < steps;
                 if (more && !fetch(next)) return false;
                 if (s >= L && !__all_sync(0xffffffffu, tc_wait(&sh.empty[la.slot], la.turn ^ 1u, gave_up, a.status, 100))) return false;
-                unpack_stage<BF16, CB, BACK>(w, left + la.slot * kLeftBytes + place.to);
+                unpack_stage<BF16, CB, EIGHT, BACK>(w, left + la.slot * kLeftBytes + place.to, base);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.written[la.slot]);
                 if (more) {
@@ -491,7 +498,11 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             }
             return true;
         };
-        bool ok = cb == 8 ? unpack(std::integral_constant<int, 8>()) : cb == 4 ? unpack(std::integral_constant<int, 4>()) : unpack(std::integral_constant<int, 2>());
+        using std::integral_constant;
+        bool ok = cb == 4   ? unpack(integral_constant<int, 4>(), std::false_type())
+                  : cb == 2 ? unpack(integral_constant<int, 2>(), std::false_type())
+                  : BF16 && a.bits == 8 ? unpack(integral_constant<int, 8>(), integral_constant<bool, BF16>())
+                                        : unpack(integral_constant<int, 8>(), std::false_type());
         if (ok) ok = __all_sync(0xffffffffu, tc_wait(&sh.plan, 0, gave_up, a.status, 101));
         if (ok && rank8 > 0) {
             if (a.early) asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -780,7 +791,7 @@ int launch_project(zipml_ctx* ctx, const ProjectArgs& a, const void* tokens_oper
     int rc = encode_map(ctx, operand_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, tokens_operand, a.depth, a.tokens, ld_operand * 2,
                         kProjDepth, pair ? nt / 2 : nt, CU_TENSOR_MAP_SWIZZLE_128B, &tokens_map);
     if (rc != ZIPML_OK) return rc;
-    rc = encode_map(ctx, CU_TENSOR_MAP_DATA_TYPE_UINT8, w->plane1, w->row_bytes, w->m, w->row_bytes, (backward ? kProjDepth : kProjRows) * a.bits / 8,
+    rc = encode_map(ctx, CU_TENSOR_MAP_DATA_TYPE_UINT8, w->plane1, w->row_bytes, w->m, w->row_bytes, (backward ? kProjDepth : kProjRows) * container_bits(a.bits) / 8,
                     backward ? kProjRows : kProjDepth, CU_TENSOR_MAP_SWIZZLE_NONE, &codes_map);
     if (rc != ZIPML_OK) return rc;
     if (backward) return launch_project_typed<true, false>(ctx, a, tokens_map, codes_map, nt, ranks, pair);

@@ -89,7 +89,7 @@ struct ShrinkArgs {
 struct ProjectArgs {
     int64_t tokens;
     int features, depth;         // rows of the product's result, length of its sums
-    int bits;                    // container bits
+    int bits;
     const float *lo, *step;      // per feature: alpha = step, beta = lo + center step; null: 1 and 1
     float center;
     const int* ids;

@@ -70,7 +70,7 @@ def weight_parts(ds):
     cb = {1: 2, 2: 2, 3: 4, 4: 4}.get(ds.bits, 8)
     shifts = torch.arange(8 // cb, device=ds.plane1.device, dtype=torch.uint8) * cb
     codes = ((ds.plane1[:, :, None] >> shifts) & ((1 << cb) - 1)).reshape(ds.m, -1)[:, :ds.n].double()
-    centre = float(1 << (cb - 1))
+    centre = float(1 << (ds.bits - 1))
     return ds.feat_lo.double() + centre * ds.feat_step.double(), ds.feat_step.double(), codes - centre
 
 
