@@ -257,7 +257,10 @@ __global__ void __launch_bounds__(32 * kShrinkWarps) shrink_kernel(ShrinkArgs a)
 // Many tokens: tiles of 128 on the tensor cores' rows, the adapters' ranks on the columns, both operands by tensor copies.  What counts is
 // that the tokens' bytes keep coming (up to eight stages of 16 KB on their way), the products are next to nothing.  The forward pass's
 // sums are one more column: 16 rows of ones lead the right operand.  A tile's adapters take `slots` at a time; a column that does not belong to
-// a token's adapter, and ranks past the last that a copy's box brings along, are not read.  A cluster's CTAs divide the columns.
+// a token's adapter, and ranks past the last that a copy's box brings along, are not read.  A cluster's CTAs divide the columns.  The
+// tensor cores cut what they add to a sum where fp32 would round, always towards zero, so a long sum loses a few units of 2^-24 for
+// every hundred products: the stages take up to eight sets of sums in turn, which are added in fp32 (8192 columns: 4.5e-6 of hidden off
+// with one set, XERR with them).
 // 8192 tokens x 8192 x 32 ranks: 200 us with the kernel above (its 16-byte loads left most of each turn waiting).
 // ---------------------------------------------------------------------------------------------
 constexpr int kTallTokens = 128;
@@ -275,7 +278,7 @@ struct TallShared {
 };
 
 struct TallShape {
-    int slots, ranks8, lead, rows, columns, stages;      // rows of the right operand; columns of tensor memory
+    int slots, ranks8, lead, rows, sums, columns, stages;   // rows of the right operand; sets of sums and columns of tensor memory
 };
 
 template <bool BF16>
@@ -379,7 +382,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
                 const uint64_t offset = (uint64_t)((uint32_t)slot * (stage_bytes / 16));
                 if (tc_elect()) {
 #pragma unroll
-                    for (int k = 0; k < kTallDepth / 16; ++k) tc_mma<false>(tmem, z_at + offset + k * 2, d_at + offset + k * 2, kind, s > 0 || k > 0);
+                    for (int k = 0; k < kTallDepth / 16; ++k) tc_mma<false>(tmem + (s % f.sums) * f.rows, z_at + offset + k * 2, d_at + offset + k * 2, kind, s >= f.sums || k > 0);
                     tc_commit<false>(&sh.empty[slot]);
                 }
                 __syncwarp();
@@ -396,22 +399,30 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
             if (ok && steps > 0) {
                 tc_fence_after();
                 const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16);
+                const auto add_sets = [&](int column, float (&y)[8]) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = 0.0f;
+                    for (int set = 0; set < min(f.sums, steps); ++set) {
+                        uint32_t v[8];
+                        tc_load8(at + set * f.rows + column, v);
+                        tc_load_wait();
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) y[k] += __uint_as_float(v[k]);
+                    }
+                };
+                float y[8];
                 if (f.lead > 0 && p == 0) {
-                    uint32_t v[8];
-                    tc_load8(at, v);
-                    tc_load_wait();
-                    sh.sum[row] = __uint_as_float(v[0]);
+                    add_sets(0, y);
+                    sh.sum[row] = y[0];
                 }
                 for (int i = 0; i < used; ++i) {
                     const bool mine = sh.distinct[p * f.slots + i] == id;
                     for (int r = 0; r < f.ranks8; r += 8) {
-                        uint32_t v[8];
-                        tc_load8(at + f.lead + i * f.ranks8 + r, v);
-                        tc_load_wait();
+                        add_sets(f.lead + i * f.ranks8 + r, y);
                         if (mine) {
 #pragma unroll
                             for (int k = 0; k < 8; ++k)
-                                if (r + k < a.rank) part[row * a.rank + r + k] = __uint_as_float(v[k]);
+                                if (r + k < a.rank) part[row * a.rank + r + k] = y[k];
                         }
                     }
                 }
@@ -562,8 +573,10 @@ static int launch_tall(zipml_ctx* ctx, const ShrinkArgs& a, int dtype, bool sums
         if (f.slots > a.requests) f.slots = a.requests;
     }
     f.rows = (f.lead + f.slots * f.ranks8 + 15) / 16 * 16;
+    f.sums = f.rows > 0 ? 512 / f.rows : 1;
+    if (f.sums > 8) f.sums = 8;
     f.columns = 32;
-    while (f.columns < f.rows) f.columns *= 2;
+    while (f.columns < f.sums * f.rows) f.columns *= 2;
     const size_t stage = kTallLeftBytes + (size_t)f.rows * 128, fixed = 1024 + sizeof(float) * kTallTokens * a.rank + sizeof(TallShared);
     f.stages = (int)((200 * 1024 - fixed) / stage);
     if (f.stages > kTallMostStages) f.stages = kTallMostStages;
