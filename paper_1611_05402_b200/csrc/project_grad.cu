@@ -40,6 +40,17 @@ __device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&x)[4], 
     asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(b0), "r"(b1));
 }
+// The same with both parts of the left factor, (low + high) x b of 8 tokens from zero, which is then added in fp32: the tensor cores cut
+// what they add to a sum where fp32 would round, always towards zero, and sums over thousands of tokens would show it.  (2048 tokens: 2.3e-6
+// of the result off when the sums stayed in the tensor cores, XGERR so.)
+__device__ __forceinline__ void add_products(float (&d)[4], const uint32_t (&high)[4], const uint32_t (&low)[4], uint32_t b0, uint32_t b1) {
+    float t[4];
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(t[0]), "=f"(t[1]), "=f"(t[2]), "=f"(t[3]) : "r"(low[0]), "r"(low[1]), "r"(low[2]), "r"(low[3]), "r"(b0), "r"(b1), "f"(0.0f));
+    mma_tf32(t, high, b0, b1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i] += t[i];
+}
 // byte i of a word, less 128 (see byte_to_float)
 __device__ __forceinline__ float centred_code(uint32_t bytes, int i) { return __uint_as_float(__byte_perm(bytes, 0x4B000000u, 0x7650 + i)) - 8388736.0f; }
 // x = high + low, both within tf32's 11 bits up to 2^-22 of x
@@ -203,8 +214,7 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* 
                             const float b0 = own ? centred_code(u0[f >> 2], f & 3) : 0.0f, b1 = own ? centred_code(u1[f >> 2], f & 3) : 0.0f;
 #pragma unroll
                             for (int m = 0; m < MT; ++m) {
-                                mma_tf32(acc[m][f], hi[m], __float_as_uint(b0), __float_as_uint(b1));
-                                mma_tf32(acc[m][f], lo[m], __float_as_uint(b0), __float_as_uint(b1));
+                                add_products(acc[m][f], hi[m], lo[m], __float_as_uint(b0), __float_as_uint(b1));
                             }
                         }
                     }
@@ -220,10 +230,8 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* 
                         const float2 b1 = a.bf16 ? unpack_pair<__nv_bfloat16>(u1[k]) : unpack_pair<__half>(u1[k]);
 #pragma unroll
                         for (int m = 0; m < MT; ++m) {
-                            mma_tf32(acc[m][2 * k], hi[m], __float_as_uint(b0.x), __float_as_uint(b1.x));
-                            mma_tf32(acc[m][2 * k], lo[m], __float_as_uint(b0.x), __float_as_uint(b1.x));
-                            mma_tf32(acc[m][2 * k + 1], hi[m], __float_as_uint(b0.y), __float_as_uint(b1.y));
-                            mma_tf32(acc[m][2 * k + 1], lo[m], __float_as_uint(b0.y), __float_as_uint(b1.y));
+                            add_products(acc[m][2 * k], hi[m], lo[m], __float_as_uint(b0.x), __float_as_uint(b1.x));
+                            add_products(acc[m][2 * k + 1], hi[m], lo[m], __float_as_uint(b0.y), __float_as_uint(b1.y));
                         }
                     }
                 }
