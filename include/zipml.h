@@ -361,7 +361,7 @@ typedef struct zipml_checkpoint {
     int64_t m, n;           /* rows, features                                                        */
     int64_t row_bytes;      /* stride of codes, a multiple of 16, >= zipml_row_bytes(n, 8)           */
     const uint8_t* codes;   /* m * row_bytes bytes, 16-byte aligned                                  */
-    const float* grids;     /* m * ceil(n / group) pairs (lo, step), 16-byte aligned                 */
+    const float* grids;     /* m * ceil(n / group) pairs (lo, step), 8-byte aligned                  */
 } zipml_checkpoint;
 
 /* zipml_checkpoint_encode: rounds X (m x n of type dtype, leading dimension ldx >= n) stochastically onto 8 bits, once, into the
@@ -404,7 +404,7 @@ typedef struct zipml_adapters {
  *             overlapping.
  *   hidden    NULL or tokens x rank floats: h_t, zero for requests without an adapter; what the backward pass needs.
  * zipml_project_backward: for dY = the loss's gradient with respect to Y, with v_t = scale_i b_i dy_t,
- *   dX[t] = W dy_t + a_i^T v_t             (tokens x inputs, dtype; NULL: not wanted)
+ *   dX[t] = W dy_t + a_i^T v_t             (tokens x inputs, dtype, not overlapping dY; NULL: not wanted)
  *   grad_a[i] = sum of v_t (x) Q(x_t)      (count x rank x inputs floats; NULL: not wanted) over the tokens of adapter i, Q(x_t) from
  *   grad_b[i] = sum of h_t (x) dy_t        `checkpoint` (its m >= tokens and n = inputs; may be NULL without grad_a); count x rank x
  *                                          outputs floats; NULL: not wanted (hidden may then be NULL)

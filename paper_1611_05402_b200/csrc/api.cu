@@ -135,7 +135,7 @@ static int check_checkpoint(const zipml_checkpoint* c) {
     if (c->group != 32 && c->group != 64 && c->group != 128 && c->group != 256) return ZIPML_ERR_UNSUPPORTED;
     if (c->m < 0 || c->n <= 0 || c->row_bytes % 16 != 0 || c->row_bytes < zipml_row_bytes(c->n, 8)) return ZIPML_ERR_INVALID_ARG;
     if (c->row_bytes > 0x7fffffffLL - 256) return ZIPML_ERR_WORKSPACE;
-    if (c->m > 0 && (!c->codes || !c->grids || !aligned16(c->codes) || !aligned16(c->grids))) return ZIPML_ERR_INVALID_ARG;
+    if (c->m > 0 && (!c->codes || !c->grids || !aligned16(c->codes) || !aligned_to(c->grids, 8))) return ZIPML_ERR_INVALID_ARG;
     return ZIPML_OK;
 }
 

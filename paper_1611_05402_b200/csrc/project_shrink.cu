@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(32 * kShrinkWarps) shrink_kernel(ShrinkArgs a)
 // a token's adapter, and ranks past the last that a copy's box brings along, are not read.  A cluster's CTAs divide the columns.  The
 // tensor cores cut what they add to a sum where fp32 would round, always towards zero, so a long sum loses a few units of 2^-24 for
 // every hundred products: the stages take up to eight sets of sums in turn, which are added in fp32 (8192 columns: 4.5e-6 of hidden off
-// with one set, XERR with them).
+// with one set, 0.7e-6 with them).
 // 8192 tokens x 8192 x 32 ranks: 200 us with the kernel above (its 16-byte loads left most of each turn waiting).
 // ---------------------------------------------------------------------------------------------
 constexpr int kTallTokens = 128;

@@ -39,11 +39,11 @@ def philox(c0, c1, c2, c3, k0, k1):
     return c
 
 
-def plain_encode(x, group, seed):
+def plain_encode(x, group, seed, first_row=0):
     """(codes, lo, step) with every operation one fp32 rounding, and the draws of the stated generator."""
     x = x.float().cpu().numpy()
     m, n = x.shape
-    rows, blocks = np.arange(m, dtype=np.uint64)[:, None], np.arange(-(-n // 8), dtype=np.uint64)[None, :]
+    rows, blocks = np.arange(first_row, first_row + m, dtype=np.uint64)[:, None], np.arange(-(-n // 8), dtype=np.uint64)[None, :]
     zero = np.zeros((m, blocks.shape[1]), dtype=np.uint64)
     words = philox(blocks + zero, rows + zero, zero, zero + np.uint64(8), seed & 0xFFFFFFFF, seed >> 32)
     draws = np.stack([h for w in words for h in (w & np.uint64(0xFFFF), w >> np.uint64(16))], 2).reshape(m, -1)[:, :n].astype(np.int64)
@@ -546,6 +546,95 @@ def test_gradients_against_differences(ctx):
     assert abs((after - at) - ((moved * da.double()).sum().item() - error)) <= 12 * rounding
 
 
+@gpu
+@pytest.mark.parametrize("tokens,inputs,outputs,rank,count,lengths", [
+    (600, 200, 328, 8, 5, [1] * 600),                  # a token a request, few adapters
+    (300, 136, 264, 16, 300, [1] * 300),               # and one of its own for each
+    (700, 600, 400, 128, 4, [100, 200, 50, 350]),      # the highest rank, several adapters in a tile
+    (520, 16500, 72, 33, 2, [260, 260]),               # long sums
+    (16, 16500, 72, 16, 2, [8, 8]),
+    (257, 72, 16500, 5, 3, [257]),
+])
+def test_extremes(ctx, tokens, inputs, outputs, rank, count, lengths):
+    p = Problem(ctx, tokens, inputs, outputs, 8, BF16, rank, count, lengths, seed=rank)
+    check_forward(ctx, p)
+    check_backward(ctx, p)
+
+
+@gpu
+def test_starts_that_are_out_of_order_or_range(ctx):
+    """Nothing outside the arrays is touched; tokens that no range holds stay as they were."""
+    p = Problem(ctx, 50, 96, 64, 8, BF16, 4, 2, [20, 30], which=[0, 1])
+    for starts in ([-7, 20, 10], [0, 100, 120], [40, 10, 2000], [60, 70, 80], [-9, -5, -1]):
+        p.starts.copy_(torch.tensor(starts, dtype=torch.int32))
+        out = torch.full((50, 64), 3.0, dtype=BF16, device=ctx.device)
+        hidden = torch.zeros(50, 4, device=ctx.device)
+        ctx.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which, out=out, hidden=hidden)
+        cp = ctx.zipml_checkpoint_encode(p.x, group=32)
+        dx = torch.full((50, 96), 3.0, dtype=BF16, device=ctx.device)
+        ctx.zipml_project_backward(p.weights, p.dy, adapters=p.adapters, starts=p.starts, which=p.which, hidden=hidden, checkpoint=cp, out=dx)
+        ctx.zipml_sync()
+        held = torch.zeros(50, dtype=torch.bool, device=ctx.device)
+        for s, e in zip(starts, starts[1:]):
+            held[max(s, 0):max(min(e, 50), 0)] = True
+        assert (out[~held] == 3.0).all() and (dx[~held] == 3.0).all()
+        assert torch.isfinite(out).all() and torch.isfinite(dx).all()
+
+
+@gpu
+def test_rows_of_a_larger_checkpoint(ctx):
+    """Gradients from some rows of a checkpoint: its arrays may be longer, and may begin anywhere that is aligned."""
+    p = Problem(ctx, 64, 96, 80, 8, BF16, 8, 2, [64], which=[1])
+    big = torch.cat([torch.randn(3, 96, device=ctx.device).to(BF16), p.x, torch.randn(5, 96, device=ctx.device).to(BF16)])
+    whole = ctx.zipml_checkpoint_encode(big, group=32, seed=9)
+    part = binding.Checkpoint(whole.codes[3:], whole.grids[3:], 69, 96, 32)
+    hidden = torch.ones(64, 8, device=ctx.device)
+    _, da, _ = ctx.zipml_project_backward(p.weights, p.dy, adapters=p.adapters, starts=p.starts, which=p.which, hidden=hidden, checkpoint=part)
+    ctx.zipml_sync()
+    ref = p.backward(hidden, part)
+    close(da, ref[2], (2.0**-20 + (80 + 64 + 64) * 2.0**-23) * ref[3] + 1e-30)
+
+
+@gpu
+def test_offsets_past_32_bits(ctx):
+    """66,000 tokens x 32,768 outputs: the last rows lie 2^31 elements on.  Their request is its own, so they are checked alone."""
+    tokens, inputs, outputs, rank, tail = 66_000, 64, 32_768, 8, 200
+    g = torch.Generator(device=ctx.device).manual_seed(1)
+    dev = ctx.device
+    weights = ctx.zipml_quantize(torch.randn(inputs, outputs, generator=g, device=dev), 4, seed=1)
+    x = torch.randn(tokens, inputs, generator=g, device=dev).to(BF16)
+    a, b = (torch.randn(2, rank, k, generator=g, device=dev).to(BF16) / 8 for k in (inputs, outputs))
+    starts = torch.tensor([0, tokens - tail, tokens], dtype=torch.int32, device=dev)
+    which = torch.tensor([0, 1], dtype=torch.int32, device=dev)
+    hidden = torch.zeros(tokens, rank, device=dev)
+    ad = binding.Adapters(a, b)
+    y = ctx.zipml_project(weights, x, adapters=ad, starts=starts, which=which, hidden=hidden)
+    cp = ctx.zipml_checkpoint_encode(x, group=32, seed=3)
+    dx, da, db = ctx.zipml_project_backward(weights, y, adapters=ad, starts=starts, which=which, hidden=hidden, checkpoint=cp)
+    ctx.zipml_sync()
+    beta, step, c = weight_parts(weights)
+    W, xt, yt = beta + step * c, x[-tail:].double(), y[-tail:].double()
+    h = xt @ a[1].double().T
+    mag = (xt.abs() @ c.abs()) * step + xt.abs().sum(1, keepdim=True) * beta.abs() + (xt.abs() @ a[1].double().abs().T) @ b[1].double().abs()
+    close(y[-tail:], xt @ W + h @ b[1].double(), half_step(BF16) * 1.01 * (xt @ W + h @ b[1].double()).abs() + (2.0**-16 + 200 * 2.0**-23) * mag)
+    v, vm = yt @ b[1].double().T, yt.abs() @ b[1].double().abs().T
+    want = yt @ W.T + v @ a[1].double()
+    mag = (yt.abs() * step) @ c.abs().T + (yt.abs() @ beta.abs())[:, None] + vm @ a[1].double().abs()
+    close(dx[-tail:], want, half_step(BF16) * 1.01 * want.abs() + (2.0**-11 + 2.0**-16 + 40_000 * 2.0**-23) * mag)
+    lo, st, codes = (t[-tail:] if t.dim() == 2 else t for t in checkpoint_values(cp))
+    close(da[1], v.T @ (lo + st * codes), (2.0**-20 + 40_000 * 2.0**-23) * (vm.T @ (st * (codes - 128).abs() + (lo + 128 * st).abs())) + 1e-30)
+    close(db[1], h.T @ yt, (2.0**-20 + 400 * 2.0**-23) * ((xt.abs() @ a[1].double().abs().T).T @ yt.abs()) + 1e-30)
+    del y, dx
+    wide = torch.randn(33_000, 65_600, generator=g, device=dev, dtype=BF16)
+    far = ctx.zipml_checkpoint_encode(wide, group=256, seed=4)
+    back = ctx.zipml_checkpoint_decode(far)
+    ctx.zipml_sync()
+    want, grids = plain_encode(wide[-2:], 256, 4, first_row=32_998)
+    assert (far.codes[-2:, :65_600].cpu().numpy() == want).all() and (far.grids[-2:].cpu().numpy() == grids).all()
+    lo, st, codes = (t[-2:] for t in checkpoint_values(binding.Checkpoint(far.codes[-2:], far.grids[-2:], 2, 65_600, 256)))
+    assert torch.equal(back[-2:].float(), (lo + st * codes).float().to(BF16).float())
+
+
 # --- how calls are made -----------------------------------------------------------------------------------------------------------
 
 @gpu
@@ -622,6 +711,34 @@ def test_captured_calls_replay(ctx, tokens):
         stream.synchronize()
         assert all(torch.equal(u, v) for u, v in zip(got, (y, hidden, dx, da, db, cp.codes)))
         del graph
+
+
+@gpu
+def test_two_contexts_at_once():
+    """Two streams, a context each, their calls interleaved: each has its own workspace."""
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    contexts = [binding.Context("cuda:0", stream=s) for s in streams]
+    problems, want = [], []
+    for i, (c, s) in enumerate(zip(contexts, streams)):
+        with torch.cuda.stream(s):
+            p = Problem(c, (40, 700)[i], 520, 390, (4, 8)[i], BF16, 16, 2, [(40, 700)[i]], which=[i], seed=i)
+            problems.append(p)
+            hidden = torch.ones(p.tokens, 16, device="cuda:0")
+            cp = c.zipml_checkpoint_encode(p.x, group=64)
+            p.kw = dict(adapters=p.adapters, starts=p.starts, which=p.which)
+            p.hidden, p.cp = hidden, cp
+            want.append([t.clone() for t in (c.zipml_project(p.weights, p.x, **p.kw), *c.zipml_project_backward(p.weights, p.dy, hidden=hidden, checkpoint=cp, **p.kw))])
+            s.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, (c, s) in enumerate(zip(contexts, streams)):
+            with torch.cuda.stream(s):
+                p = problems[i]
+                got[i].append((c.zipml_project(p.weights, p.x, **p.kw), *c.zipml_project_backward(p.weights, p.dy, hidden=p.hidden, checkpoint=p.cp, **p.kw)))
+    for i, c in enumerate(contexts):
+        c.zipml_sync()
+        assert all(torch.equal(u, v) for r in got[i] for u, v in zip(want[i], r))
+        c.close()
 
 
 @gpu
