@@ -125,10 +125,11 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* 
         const auto issue = [&] {                           // (into the slot that was read longest ago, by this warp)
             if (ahead.i >= segments) return;
             const uint32_t slot = issued % SLOTS;
-            if (lane == 0) {
+            if (tc_elect()) {
                 mbar_arrive_expect_tx(&sh.full[warp][slot], kGradSlotBytes);
                 tc_copy_2d(smem_u32(slots + slot * kGradSlotBytes), map, col0, sh.begin[ahead.i] + ahead.c * kGradChunk, &sh.full[warp][slot]);
             }
+            __syncwarp();
             ++issued;
             step(ahead);
         };

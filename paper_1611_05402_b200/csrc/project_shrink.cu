@@ -278,7 +278,10 @@ struct TallShared {
 };
 
 struct TallShape {
-    int slots, ranks8, lead, rows, sums, columns, stages;   // rows of the right operand; sets of sums and columns of tensor memory
+    int slots, ranks8, lead, rows, columns, stages;      // rows of the right operand; columns of tensor memory
+    // columns of a pass with so many adapters, and sets of sums that tensor memory has room for
+    __device__ __forceinline__ int pass_columns(int used) const { return (lead + used * ranks8 + 15) & ~15; }
+    __device__ __forceinline__ int pass_sets(int used) const { return min(8, columns / max(pass_columns(used), 16)); }
 };
 
 template <bool BF16>
@@ -292,7 +295,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
     TallShared& sh = *reinterpret_cast<TallShared*>(part + kTallTokens * a.rank);
     cg::cluster_group cluster = cg::this_cluster();
     const int crank = (int)cluster.block_rank(), cranks = (int)cluster.num_blocks();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // (known to be the same for a whole warp)
     const int64_t t0 = (int64_t)(blockIdx.x / cranks) * kTallTokens;
     const int all_steps = (a.columns + kTallDepth - 1) / kTallDepth, per = (all_steps + cranks - 1) / cranks;
     const int step0 = min(crank * per, all_steps), steps = min(per, all_steps - step0);
@@ -346,31 +349,35 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
     const int passes = max(f.slots > 0 ? (sh.count + f.slots - 1) / f.slots : 0, f.lead > 0 ? 1 : 0);
 
     if (warp == 0) {
-        if (lane == 0) {
-            int n = 0;                                                                // stages of all passes
-            bool ok = true;
-            for (int p = 0; ok && p < passes; ++p) {
-                const int used = min(f.slots, sh.count - p * f.slots);
-                for (int s = 0; s < steps; ++s, ++n) {
-                    const int slot = n % f.stages;
-                    if (n >= f.stages && !tc_wait(&sh.empty[slot], (n / f.stages - 1) & 1, gave_up, a.status, 110)) { ok = false; break; }
-                    mbar_arrive_expect_tx(&sh.full[slot], kTallLeftBytes + (uint32_t)(max(used, 0) * f.ranks8 * 128));
-                    const uint32_t at = smem_u32(ring + slot * stage_bytes);
+        int n = 0;                                                                    // stages of all passes
+        bool ok = true;
+        const uint32_t first = smem_u32(ring);
+        for (int p = 0; ok && p < passes; ++p) {
+            const int used = max(min(f.slots, sh.count - p * f.slots), 0);
+            for (int s = 0, slot = n % f.stages; s < steps; ++s, ++n, slot = slot + 1 == f.stages ? 0 : slot + 1) {
+                if (n >= f.stages) ok = __all_sync(0xffffffffu, tc_wait(&sh.empty[slot], (n / f.stages - 1) & 1, gave_up, a.status, 110));
+                if (!ok) break;
+                const uint32_t at = first + slot * stage_bytes;
+                if (tc_elect()) {
+                    mbar_arrive_expect_tx(&sh.full[slot], kTallLeftBytes + (uint32_t)(used * f.ranks8 * 128));
                     tc_copy_2d(at, &z_map, (step0 + s) * kTallDepth, (int)t0, &sh.full[slot]);
                     for (int i = 0; i < used; ++i)
                         tc_copy_2d(at + kTallLeftBytes + (f.lead + i * f.ranks8) * 128, &down_map, (step0 + s) * kTallDepth, sh.distinct[p * f.slots + i] * a.rank, &sh.full[slot]);
                 }
+                __syncwarp();
             }
-            if (!ok)
-                for (int i = max(0, n - f.stages); i < n; ++i) tc_drain(&sh.full[i % f.stages], (i / f.stages) & 1);
         }
+        if (!ok && lane == 0)
+            for (int i = max(0, n - f.stages); i < n; ++i) tc_drain(&sh.full[i % f.stages], (i / f.stages) & 1);
+        __syncwarp();
     } else if (warp == 1) {
         int n = 0;
         bool ok = true;
         const uint64_t z_at = tc_operand(smem_u32(ring), 16, 1024), d_at = tc_operand(smem_u32(ring + kTallLeftBytes), 16, 1024);
         for (int p = 0; p < passes; ++p) {                                            // (every pass's barrier, whether or not a wait has given up)
             const int used = max(min(f.slots, sh.count - p * f.slots), 0);
-            const uint32_t kind = tc_kind(BF16, false, kTallTokens, (f.lead + used * f.ranks8 + 15) & ~15);
+            const int n16 = f.pass_columns(used), sets = f.pass_sets(used);
+            const uint32_t kind = tc_kind(BF16, false, kTallTokens, n16);
             // (the pass before has to have been read out of tensor memory)
             if (p > 0) asm volatile("bar.sync 1, %0;" ::"n"(32 * 5) : "memory");
             tc_fence_after();
@@ -382,7 +389,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
                 const uint64_t offset = (uint64_t)((uint32_t)slot * (stage_bytes / 16));
                 if (tc_elect()) {
 #pragma unroll
-                    for (int k = 0; k < kTallDepth / 16; ++k) tc_mma<false>(tmem + (s % f.sums) * f.rows, z_at + offset + k * 2, d_at + offset + k * 2, kind, s >= f.sums || k > 0);
+                    for (int k = 0; k < kTallDepth / 16; ++k) tc_mma<false>(tmem + (s % sets) * n16, z_at + offset + k * 2, d_at + offset + k * 2, kind, s >= sets || k > 0);
                     tc_commit<false>(&sh.empty[slot]);
                 }
                 __syncwarp();
@@ -399,12 +406,13 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
             if (ok && steps > 0) {
                 tc_fence_after();
                 const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16);
+                const int n16 = f.pass_columns(used), sets = min(f.pass_sets(used), steps);
                 const auto add_sets = [&](int column, float (&y)[8]) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) y[k] = 0.0f;
-                    for (int set = 0; set < min(f.sums, steps); ++set) {
+                    for (int set = 0; set < sets; ++set) {
                         uint32_t v[8];
-                        tc_load8(at + set * f.rows + column, v);
+                        tc_load8(at + set * n16 + column, v);
                         tc_load_wait();
 #pragma unroll
                         for (int k = 0; k < 8; ++k) y[k] += __uint_as_float(v[k]);
@@ -568,15 +576,12 @@ static int launch_tall(zipml_ctx* ctx, const ShrinkArgs& a, int dtype, bool sums
     f.lead = sums ? 16 : 0;
     f.ranks8 = (a.rank + 7) / 8 * 8;
     if (a.down) {
-        f.slots = f.ranks8 >= 64 ? 1 : 64 / f.ranks8;
+        f.slots = 128 / f.ranks8;                        // (a tile that needs a second pass takes twice as long, and all wait for it)
         if (f.slots > a.adapters) f.slots = a.adapters;
         if (f.slots > a.requests) f.slots = a.requests;
     }
     f.rows = (f.lead + f.slots * f.ranks8 + 15) / 16 * 16;
-    f.sums = f.rows > 0 ? 512 / f.rows : 1;
-    if (f.sums > 8) f.sums = 8;
-    f.columns = 32;
-    while (f.columns < f.sums * f.rows) f.columns *= 2;
+    f.columns = f.rows > 0 ? 512 : 32;
     const size_t stage = kTallLeftBytes + (size_t)f.rows * 128, fixed = 1024 + sizeof(float) * kTallTokens * a.rank + sizeof(TallShared);
     f.stages = (int)((200 * 1024 - fixed) / stage);
     if (f.stages > kTallMostStages) f.stages = kTallMostStages;
