@@ -101,16 +101,33 @@ __device__ __forceinline__ void lane_range(const uint32_t (&w)[kLaneFeatures * s
     }
 }
 
+// Unit u of `per` a row, u = first, first + stride, ...: its row and place there, without a division a turn.
+struct RowUnits {
+    int64_t row;
+    int place, per, step_place;
+    int64_t step_row;
+    __device__ __forceinline__ RowUnits(int64_t first, int64_t stride, int per_row) : per(per_row) {
+        row = first / per;
+        place = (int)(first - row * per);
+        step_row = stride / per;
+        step_place = (int)(stride - step_row * per);
+    }
+    __device__ __forceinline__ void next() {
+        row += step_row;
+        place += step_place;
+        if (place >= per) { place -= per; ++row; }
+    }
+};
+
 template <typename T>
 __global__ void __launch_bounds__(32 * kEncodeWarps) checkpoint_encode_kernel(const __grid_constant__ EncodeArgs a) {
     constexpr int W = kLaneFeatures * sizeof(T) / 4;
     const int lane = threadIdx.x & 31;
-    const int64_t units = a.m * a.segments;
     const int lanes = a.group / kLaneFeatures;
     bool bad = false;
-    for (int64_t u = (int64_t)blockIdx.x * kEncodeWarps + (threadIdx.x >> 5); u < units; u += (int64_t)gridDim.x * kEncodeWarps) {
-        const int64_t row = u / a.segments;
-        const int j = (int)(u - row * a.segments) * kWarpFeatures + lane * kLaneFeatures;
+    for (RowUnits u((int64_t)blockIdx.x * kEncodeWarps + (threadIdx.x >> 5), (int64_t)gridDim.x * kEncodeWarps, a.segments); u.row < a.m; u.next()) {
+        const int64_t row = u.row;
+        const int j = u.place * kWarpFeatures + lane * kLaneFeatures;
         const int count = min(max(a.n - j, 0), kLaneFeatures);
         uint32_t w[W] = {};
         float lo = INFINITY, hi = -INFINITY;
@@ -165,10 +182,9 @@ __global__ void __launch_bounds__(32 * kEncodeWarps) checkpoint_encode_kernel(co
 template <typename T>
 __global__ void __launch_bounds__(256) checkpoint_decode_kernel(const uint8_t* codes, int64_t row_bytes, const float2* grids, int groups, int group_shift, int64_t m,
                                                                 int n, int blocks, T* x, int64_t ldx, int wide) {
-    const int64_t units = m * blocks;
-    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
-        const int64_t row = u / blocks;
-        const int j = (int)(u - row * blocks) * kLaneFeatures;
+    for (RowUnits u((int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256, blocks); u.row < m; u.next()) {
+        const int64_t row = u.row;
+        const int j = u.place * kLaneFeatures;
         const uint4 c = *reinterpret_cast<const uint4*>(codes + row * row_bytes + j);
         const float2 g = grids[row * groups + (j >> group_shift)];
         const int count = min(n - j, kLaneFeatures);
