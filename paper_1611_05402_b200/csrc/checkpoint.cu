@@ -14,7 +14,8 @@ namespace zipml {
 //   the probability of t's fraction (rounded up to 2^-16: the mean is off by at most 2^-16 of a step).
 // Bound by instructions, the generator's 64-bit products first: 16 random bits a value instead of the quantizers' 24, the round keys
 // from the host, minimum and maximum of 16-bit types in pairs, and 16 features a lane for one butterfly and two divisions.
-// XENCODE
+// 16,384 x 8,192 bf16 137 us (3.0 TB/s in and out; 28 instructions a value, three quarters of the issue slots taken), 259 with 8 features a
+// lane, keys worked out a round and ranges one by one; 2,047 x 4,096 fp16 11 us.
 // ---------------------------------------------------------------------------------------------
 constexpr int kEncodeWarps = 8;
 constexpr int kLaneFeatures = 16;
@@ -178,7 +179,7 @@ __global__ void __launch_bounds__(32 * kEncodeWarps) checkpoint_encode_kernel(co
     if (bad) set_status(a.status, ZIPML_ERR_NONFINITE, 92);
 }
 
-// A thread takes 16 codes; bound by HBM.
+// A thread takes 16 codes; bound by HBM: 16,384 x 8,192 to bf16 68 us, 6.0 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(256) checkpoint_decode_kernel(const uint8_t* codes, int64_t row_bytes, const float2* grids, int groups, int group_shift, int64_t m,
                                                                 int n, int blocks, T* x, int64_t ldx, int wide) {

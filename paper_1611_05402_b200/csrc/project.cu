@@ -12,19 +12,27 @@ namespace zipml {
 namespace cg = cooperative_groups;
 
 // ---------------------------------------------------------------------------------------------
-// A CTA makes 128 features x NT tokens.  The features stand on the product's 128 rows and the tokens on its columns, so one
-// kernel serves from a token (16 columns, the codes' bytes are what counts) to thousands.  Per 64 of the depth:
-//   codes     a tensor copy brings the packed codes; groups of four warps, each with a stage of its own, turn them into 16-bit whole numbers code - 2^(bits-1), which are exact, and
-//             lay them out as the product's left operand.  Forward: a code row is one depth and holds the features (MN-major
-//             operand); backward: a code row is a feature (K-major).
-//   tokens    a tensor copy lays the right operand out itself.
-//   product   one thread issues 128 x NT x 16 four times, sums in tensor memory.
+// A CTA makes 128 features x NT tokens, a pair of CTAs 256 x 256.  The features stand on the product's rows and the tokens on its columns, so
+// one kernel serves from a token (16 columns, the codes' bytes are what counts) to thousands.  Per 64 of the depth, a stage:
+//   codes     A tensor copy brings the packed codes.  Groups of four warps, each with a stage of its own, turn them into 16-bit whole numbers
+//             code - 2^(bits-1), which are exact, and lay them out as the product's left operand; a fifth warp makes a group's stores
+//             visible to the tensor cores.  Forward: a code row is one depth and holds the features (MN-major operand);
+//             backward: a code row is a feature (K-major).
+//   tokens    A tensor copy lays the right operand out itself.  Of a pair each CTA brings half of it, and the tensor cores share it.
+//   product   One lane issues 128 (256) x NT x 16 four times, sums in tensor memory.
 // The adapters then take further stages: the ranks of the tile's adapters, each padded to a multiple of 8, follow one another as a depth of
 // their own, 32 a stage.  up_i's rows are the left operand as they lie, hidden the right one, in two 16-bit parts (high and low: 16 or more
 // bits), zero for tokens of other adapters, over the 16-token windows that hold the stage's tokens.  Their sums have columns of their own,
 // since the grids' steps do not apply to them.
 // The epilogue takes steps, sums and scales together in fp32 and rounds once.  With few tokens a cluster's CTAs divide the depth and
 // add their results through each other's shared memory in a fixed order.
+//
+// What bounds it: shared memory.  A stage of a pair's CTA writes 16 KB of tokens and 4 or 8 KB of codes, reads those, writes 16 KB of left
+// operand, and the tensor cores read 32 KB: some 600 cycles at 128 bytes each, and it takes 560 to 590, where the product alone takes 512.  A
+// tile then waits for its start (2,000 cycles), the adapters (4,500) and the epilogue (9,000).  8192 x 8192 x 8192, 4 bits, rank 32: 800 us,
+// 1.37 PFLOP/s; 4096 tokens x 4096 x 16384, 8 bits, rank 16: 475 us; backward 8192 x 8192 x 8192, 8 bits: 860 us.  With single CTAs of 128
+// x 256, which read every token twice as often from L2, the first took 990 us.  Few tokens: 470 to 530 cycles a stage against the 130 that the
+// codes' bytes would take; without the unpacking 285.
 // ---------------------------------------------------------------------------------------------
 constexpr int kProjRows = 128;                // features of a CTA
 constexpr int kProjDepth = 64;                // depth of a stage: 128 bytes of 16-bit operand
@@ -756,10 +764,11 @@ static int launch_project_as(zipml_ctx* ctx, const ProjectArgs& a, const CUtenso
     return cuda_status(e != cudaSuccess ? e : cudaGetLastError());
 }
 
-// Tokens of a tile and CTAs that divide the depth, by the cycles that a wave of tiles should take: a stage is bound by shared memory
-// (both operands are read by the tensor core and the left one written by the unpacking warps, 128 bytes a cycle: NT + 256), a tile also pays for
-// its start, its epilogue and, where the depth is divided, the exchange.
-// Pairs of CTAs halve what a stage of 256 tokens reads and keeps of them (NT / 2 + 256, the product's own 2 NT at least).
+// Tokens of a tile and CTAs that divide the depth, by the cycles that the waves of tiles should take, as measured: 480 a stage and 1 for every
+// token of a single CTA's tile, 580 for a pair's, and for a tile's start, adapters and epilogue 4,500 and 42 for every token, where the
+// depth is divided 1,500 more.  (Whole calls: 64 tokens x 4096 x 14336
+// 44 us with tiles of 64, 45 with 128, 98 with 16; 200 x 4096 x 4096 33 us with the depth divided, 38 without; 1000 x 4096 x 4096
+// 51 us by pairs, 68 with tiles of 128, 96 with 64.)
 static void project_shape(const zipml_ctx* ctx, const ProjectArgs& a, int* tokens, int* ranks, bool* pair) {
     const int64_t feature_tiles = (a.features + kProjRows - 1) / kProjRows, steps = (a.depth + kProjDepth - 1) / kProjDepth;
     double best = 0.0;
@@ -769,7 +778,7 @@ static void project_shape(const zipml_ctx* ctx, const ProjectArgs& a, int* token
             if (nt == 256 && a.up && a.tokens < (int64_t)a.requests * 32) break;      // (a pair takes all of a tile's columns for each adapter)
             const int64_t ctas = (a.tokens + nt - 1) / nt * feature_tiles * r;
             const int64_t waves = (ctas + ctx->sm_count - 1) / ctx->sm_count;
-            const double cycles = (double)waves * ((double)((steps + r - 1) / r) * (nt == 256 ? 600 : nt + 256) + 3000 + nt * 16 + (r > 1 ? 1500 : 0));
+            const double cycles = (double)waves * ((double)((steps + r - 1) / r) * (nt == 256 ? 580 : 480 + nt) + 4500 + nt * 42 + (r > 1 ? 1500 : 0));
             if (best == 0.0 || cycles < best) { best = cycles; *tokens = nt; *ranks = r; }
         }
     *pair = *tokens == 256;
