@@ -26,6 +26,7 @@ constexpr uint32_t kGradSlotBytes = kGradChunk * 128;
 constexpr int kGradBatch = kGradThreads;                // requests that are looked at together
 // Slots of a warp: two CTAs of an SM for up to 16 ranks, one (by its registers) for 32.
 __host__ __device__ constexpr int grad_slots(int mt) { return mt == 1 ? 3 : 6; }
+static_assert(3 * kGradSlotBytes >= 16 * 128 * sizeof(float) && 6 * kGradSlotBytes >= 32 * 128 * sizeof(float), "a warp's sums fit its slots");
 constexpr int kGradMostSlots = 6;
 
 struct GradShared {
@@ -51,6 +52,17 @@ __device__ __forceinline__ void add_products(float (&d)[4], const uint32_t (&hig
 #pragma unroll
     for (int i = 0; i < 4; ++i) d[i] += t[i];
 }
+// The same where the right factor has two parts too (the product of the low ones is below what is kept).
+__device__ __forceinline__ void add_products(float (&d)[4], const uint32_t (&high)[4], const uint32_t (&low)[4], float b0, float b1) {
+    const uint32_t h0 = __float_as_uint(b0) & 0xffffe000u, h1 = __float_as_uint(b1) & 0xffffe000u;
+    float t[4];
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(t[0]), "=f"(t[1]), "=f"(t[2]), "=f"(t[3]) : "r"(low[0]), "r"(low[1]), "r"(low[2]), "r"(low[3]), "r"(h0), "r"(h1), "f"(0.0f));
+    mma_tf32(t, high, __float_as_uint(b0 - __uint_as_float(h0)), __float_as_uint(b1 - __uint_as_float(h1)));
+    mma_tf32(t, high, h0, h1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i] += t[i];
+}
 // byte i of a word, less 128 (see byte_to_float)
 __device__ __forceinline__ float centred_code(uint32_t bytes, int i) { return __uint_as_float(__byte_perm(bytes, 0x4B000000u, 0x7650 + i)) - 8388736.0f; }
 // x = high + low, both within tf32's 11 bits up to 2^-22 of x
@@ -59,34 +71,38 @@ __device__ __forceinline__ void split_tf32(float x, uint32_t& high, uint32_t& lo
     low = __float_as_uint(x - __uint_as_float(high));
 }
 
-// The left factors and grids of 8 tokens, as a lane needs them: ranks g and g + 8 of each block, tokens 2 q and 2 q + 1.
-template <int GROUPS, int MT>
+// What stands on the right: the values of dy; codes on one grid a token for the whole block (groups of 128 features and more), whose step goes to
+// the left and whose lower end is summed apart; or codes of narrower groups, as the values they stand for.
+enum GradRight { kDy = 0, kCodes = 1, kValues = 2 };
+
+// The left factors of 8 tokens and their grids, as a lane needs them: ranks g and g + 8 of each block, tokens 2 q and 2 q + 1.
+template <int MT>
 struct GradLeft {
     float v[MT][4];
-    float2 grid[GROUPS][2];
+    float2 grid[2];
 };
 
-// GROUPS: grids that a block of columns lies in (1, or 4 where groups may be narrower than 128), 0 for the values of dy.  MT: blocks of 16
-// ranks, 1 or 2 (registers); higher ranks read the rows once for each 32.
-template <int GROUPS, int MT>
+// MT: blocks of 16 ranks, 1 or 2 (registers); higher ranks read the rows once for each 32.
+template <int RIGHT, int MT>
 __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* map, int adapter, int block, int r0, uint8_t* ring, GradShared& sh,
                                           cg::cluster_group& cluster) {
-    constexpr bool CODES = GROUPS > 0;
-    constexpr int GR = CODES ? GROUPS : 1, NF = CODES ? 16 : 8;            // NF: columns of a lane's 16 bytes
+    constexpr bool CODES = RIGHT != kDy;
+    constexpr int NF = CODES ? 16 : 8;                     // columns of a lane's 16 bytes
     constexpr int SLOTS = grad_slots(MT);
-    using Left = GradLeft<GR, MT>;
+    using Left = GradLeft<MT>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int ranks = (int)cluster.num_blocks(), crank = (int)cluster.block_rank();
     const int columns = CODES ? a.inputs : a.outputs;
     const int col0 = block * NF * 8, lane_col = col0 + g * NF;
     const bool copied = CODES || a.dy_copied;
     const float* left = CODES ? a.v : a.hidden;
-    const int per = GROUPS == 4 ? 128 / a.group : 1;       // grids in the block
+    const int grid_at = CODES ? (RIGHT == kValues ? min(lane_col, columns - 1) : col0) / a.group : 0;
     volatile int* gave_up = &sh.gave_up;
     uint8_t* slots = ring + warp * SLOTS * kGradSlotBytes;
     float acc[MT][NF][4] = {};
-    float base[MT][GR][2] = {};
+    float base[MT][2] = {};
     const int others = ranks * kGradWarps, me = crank * kGradWarps + warp; // (a power of two of warps take the chunks in turn)
+    bool any = false;                                      // has this adapter tokens?
     int turn = 0;                                          // chunks of the batches so far, of all warps
     uint32_t taken = 0, issued = 0;                        // of this one
     for (int first = 0; first < a.requests; first += kGradBatch) {
@@ -109,6 +125,7 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* 
         }
         __syncthreads();
         const int segments = sh.segments;
+        any |= segments > 0;
         struct Cursor { int i, c, turn; };                 // chunk c of range i, the turn-th of all warps' chunks
         const auto settle = [&](Cursor& at) {              // on to the next chunk that is this warp's
             while (at.i < segments) {
@@ -150,13 +167,9 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* 
             }
             if constexpr (CODES) {
                 const float2 none = make_float2(0.0f, 0.0f);
-#pragma unroll
-                for (int k = 0; k < GR; ++k) {
-                    const bool there = k < per && col0 + k * a.group < columns;
-                    const int64_t at = (int64_t)t * a.groups + (col0 + k * a.group) / a.group;
-                    l.grid[k][0] = there && in0 ? a.grids[at] : none;
-                    l.grid[k][1] = there && in1 ? a.grids[at + a.groups] : none;
-                }
+                const float2* p = a.grids + (int64_t)t * a.groups + grid_at;
+                l.grid[0] = in0 ? p[0] : none;
+                l.grid[1] = in1 ? p[a.groups] : none;
             }
         };
         Left next;
@@ -192,31 +205,31 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* 
                 }
                 const uint32_t u0[4] = {w0.x, w0.y, w0.z, w0.w}, u1[4] = {w1.x, w1.y, w1.z, w1.w};
                 if constexpr (CODES) {
-                    // Where the block holds several groups, each takes a product of its own, with v times its step on the left and the other
-                    // groups' columns zero on the right.
+                    const float2 g0 = l.grid[0], g1 = l.grid[1];
+                    uint32_t hi[MT][4], lo[MT][4];
 #pragma unroll
-                    for (int k = 0; k < GR; ++k) {
-                        if (k >= per) break;
-                        const float2 g0 = l.grid[k][0], g1 = l.grid[k][1];
-                        const float m0 = fmaf(128.0f, g0.y, g0.x), m1 = fmaf(128.0f, g1.y, g1.x);
-                        const bool own = GR == 1 || (g * NF) / a.group == k;
-                        uint32_t hi[MT][4], lo[MT][4];
-#pragma unroll
-                        for (int m = 0; m < MT; ++m) {
-                            split_tf32(l.v[m][0] * g0.y, hi[m][0], lo[m][0]);
-                            split_tf32(l.v[m][1] * g0.y, hi[m][1], lo[m][1]);
-                            split_tf32(l.v[m][2] * g1.y, hi[m][2], lo[m][2]);
-                            split_tf32(l.v[m][3] * g1.y, hi[m][3], lo[m][3]);
-                            base[m][k][0] += fmaf(l.v[m][0], m0, l.v[m][2] * m1);
-                            base[m][k][1] += fmaf(l.v[m][1], m0, l.v[m][3] * m1);
+                    for (int m = 0; m < MT; ++m) {
+                        const float s0 = RIGHT == kCodes ? g0.y : 1.0f, s1 = RIGHT == kCodes ? g1.y : 1.0f;
+                        split_tf32(l.v[m][0] * s0, hi[m][0], lo[m][0]);
+                        split_tf32(l.v[m][1] * s0, hi[m][1], lo[m][1]);
+                        split_tf32(l.v[m][2] * s1, hi[m][2], lo[m][2]);
+                        split_tf32(l.v[m][3] * s1, hi[m][3], lo[m][3]);
+                        if constexpr (RIGHT == kCodes) {
+                            const float m0 = fmaf(128.0f, g0.y, g0.x), m1 = fmaf(128.0f, g1.y, g1.x);
+                            base[m][0] += fmaf(l.v[m][0], m0, l.v[m][2] * m1);
+                            base[m][1] += fmaf(l.v[m][1], m0, l.v[m][3] * m1);
                         }
+                    }
 #pragma unroll
-                        for (int f = 0; f < NF; ++f) {
-                            const float b0 = own ? centred_code(u0[f >> 2], f & 3) : 0.0f, b1 = own ? centred_code(u1[f >> 2], f & 3) : 0.0f;
+                    for (int f = 0; f < NF; ++f) {
+                        if constexpr (RIGHT == kCodes) {
+                            const uint32_t b0 = __float_as_uint(centred_code(u0[f >> 2], f & 3)), b1 = __float_as_uint(centred_code(u1[f >> 2], f & 3));
 #pragma unroll
-                            for (int m = 0; m < MT; ++m) {
-                                add_products(acc[m][f], hi[m], lo[m], __float_as_uint(b0), __float_as_uint(b1));
-                            }
+                            for (int m = 0; m < MT; ++m) add_products(acc[m][f], hi[m], lo[m], b0, b1);
+                        } else {
+                            const float b0 = fmaf(byte_to_float(u0[f >> 2], f & 3), g0.y, g0.x), b1 = fmaf(byte_to_float(u1[f >> 2], f & 3), g1.y, g1.x);
+#pragma unroll
+                            for (int m = 0; m < MT; ++m) add_products(acc[m][f], hi[m], lo[m], b0, b1);
                         }
                     }
                 } else {
@@ -247,66 +260,62 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* 
     }
     if (*gave_up && lane == 0)                             // (copies that nobody has waited for)
         for (; taken < issued; ++taken) tc_drain(&sh.full[warp][taken % SLOTS], (taken / SLOTS) & 1);
-    if constexpr (CODES) {
+    if constexpr (RIGHT == kCodes) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int k = 0; k < GR; ++k)
+            for (int i = 0; i < 2; ++i) {
+                float s = base[m][i];
+                s += __shfl_xor_sync(0xffffffffu, s, 1);
+                s += __shfl_xor_sync(0xffffffffu, s, 2);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float s = base[m][k][i];
-                    s += __shfl_xor_sync(0xffffffffu, s, 1);
-                    s += __shfl_xor_sync(0xffffffffu, s, 2);
-                    base[m][k][i] = s;
-                }
-            // column n of the product's blocks is lane n's 16 codes: columns 2 q and 2 q + 1 here
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int mine = GR == 1 ? 0 : ((2 * q + half) * NF) / a.group;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float s = base[m][0][i];
-#pragma unroll
-                    for (int k = 1; k < GR; ++k)
-                        if (mine == k) s = base[m][k][i];
-#pragma unroll
-                    for (int f = 0; f < NF; ++f) acc[m][f][2 * i + half] += s;
+                for (int f = 0; f < NF; ++f) {
+                    acc[m][f][2 * i] += s;
+                    acc[m][f][2 * i + 1] += s;
                 }
             }
-        }
     }
-    // Sums over the warps, then over the CTAs, 16 ranks at a time: [warp][rank][column] in the ring's place, 16 bytes at a position that the
-    // eight lanes of a store share no bank in.
     constexpr int C = NF * 8;
-    float* out = CODES ? a.grad_down : a.grad_up;
+    float* out = (CODES ? a.grad_down : a.grad_up) + ((int64_t)adapter * a.rank + r0) * columns + col0;
+    const int most = min(16 * MT, a.rank - r0);
+    if (!any) {                                            // (for all CTAs of the cluster)
+        for (int i = crank * kGradThreads + threadIdx.x; i < most * C; i += ranks * kGradThreads)
+            if (col0 + i % C < columns) out[(int64_t)(i / C) * columns + i % C] = 0.0f;
+        return;
+    }
+    // Sums over the warps, then over the CTAs: [warp][rank][column] in the slots' place, 16 bytes at a position that the eight lanes of a
+    // store share no bank in.
     float* sums = reinterpret_cast<float*>(ring);
     const auto place = [](int r, int col) { return r * C + (((col >> 2) ^ ((col >> (CODES ? 5 : 4)) & 3) ^ ((r & 1) << 2)) << 2) + (col & 3); };
+    __syncthreads();                                       // (the slots have been read)
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        __syncthreads();                                   // (the ring has been read, the sums before have been taken)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int f = 0; f < NF; f += 4)
-                *reinterpret_cast<float4*>(sums + warp * 16 * C + place(g + 8 * (i >> 1), (2 * q + (i & 1)) * NF + f)) =
+                *reinterpret_cast<float4*>(sums + warp * 16 * MT * C + place(m * 16 + g + 8 * (i >> 1), (2 * q + (i & 1)) * NF + f)) =
                     make_float4(acc[m][f][i], acc[m][f + 1][i], acc[m][f + 2][i], acc[m][f + 3][i]);
-        __syncthreads();
-        for (int i = threadIdx.x; i < 16 * C; i += kGradThreads) {
-            float s = sums[i];
+    __syncthreads();
+    const auto of_warps = [&](int i) {
+        float s = sums[i];
 #pragma unroll
-            for (int w = 1; w < kGradWarps; ++w) s += sums[w * 16 * C + i];
-            sums[i] = s;
-        }
-        cluster.sync();
-        const int most = min(16, a.rank - r0 - m * 16);
-        for (int i = crank * kGradThreads + threadIdx.x; i < most * C; i += ranks * kGradThreads) {
-            const int r = i / C, col = i % C;
-            float s = 0.0f;
-            for (int c = 0; c < ranks; ++c) s += cluster.map_shared_rank(sums, c)[place(r, col)];
-            if (col0 + col < columns) out[((int64_t)adapter * a.rank + r0 + m * 16 + r) * columns + col0 + col] = s;
-        }
-        cluster.sync();
+        for (int w = 1; w < kGradWarps; ++w) s += sums[w * 16 * MT * C + i];
+        return s;
+    };
+    if (ranks == 1) {
+        for (int i = threadIdx.x; i < most * C; i += kGradThreads)
+            if (col0 + i % C < columns) out[(int64_t)(i / C) * columns + i % C] = of_warps(place(i / C, i % C));
+        return;
     }
+    for (int i = threadIdx.x; i < 16 * MT * C; i += kGradThreads) sums[i] = of_warps(i);
+    cluster.sync();
+    for (int i = crank * kGradThreads + threadIdx.x; i < most * C; i += ranks * kGradThreads) {
+        float s = 0.0f;
+        for (int c = 0; c < ranks; ++c) s += cluster.map_shared_rank(sums, c)[place(i / C, i % C)];
+        if (col0 + i % C < columns) out[(int64_t)(i / C) * columns + i % C] = s;
+    }
+    cluster.sync();
 }
 
 template <int MT>
@@ -321,9 +330,9 @@ __global__ void __launch_bounds__(kGradThreads, MT == 1 ? 2 : 1) grad_kernel(Gra
     }
     cg::cluster_group cluster = cg::this_cluster();
     const int block = blockIdx.x / cluster.num_blocks(), adapter = blockIdx.y, r0 = blockIdx.z * MT * 16;
-    if (block >= a.down_blocks) grad_pass<0, MT>(a, &dy_map, adapter, block - a.down_blocks, r0, ring, sh, cluster);
-    else if (a.group >= 128) grad_pass<1, MT>(a, &codes_map, adapter, block, r0, ring, sh, cluster);
-    else grad_pass<4, MT>(a, &codes_map, adapter, block, r0, ring, sh, cluster);
+    if (block >= a.down_blocks) grad_pass<kDy, MT>(a, &dy_map, adapter, block - a.down_blocks, r0, ring, sh, cluster);
+    else if (a.group >= 128) grad_pass<kCodes, MT>(a, &codes_map, adapter, block, r0, ring, sh, cluster);
+    else grad_pass<kValues, MT>(a, &codes_map, adapter, block, r0, ring, sh, cluster);
 }
 
 template <int MT>
@@ -333,7 +342,9 @@ static int launch_grad_as(zipml_ctx* ctx, const GradArgs& a, const CUtensorMap& 
     const int rc = allow_shared(ctx, reinterpret_cast<const void*>(&grad_kernel<MT>), smem);
     if (rc != ZIPML_OK) return rc;
     int ranks = 1;
-    while (ranks < 8 && (int64_t)blocks * a.adapters * passes * ranks < 2 * ctx->sm_count && (int64_t)ranks * kGradWarps * kGradChunk < a.tokens) ranks *= 2;
+    // (as many CTAs as the GPU holds at a time: two an SM for up to 16 ranks, one for more)
+    const int busy = a.adapters < a.requests ? a.adapters : a.requests;
+    while (ranks < 8 && (int64_t)blocks * busy * passes * ranks < (MT == 1 ? 2 : 1) * ctx->sm_count && (int64_t)ranks * kGradWarps * kGradChunk < a.tokens) ranks *= 2;
     if (a.adapters > 65535 || (int64_t)blocks * ranks > 0x7fffffffLL) return ZIPML_ERR_WORKSPACE;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(blocks * ranks), (unsigned)a.adapters, (unsigned)passes);
