@@ -274,7 +274,7 @@ struct TallShared {
     uint32_t tmem;
     int gave_up;
     int ids[kTallTokens], distinct[kTallTokens], count;
-    float sum[kTallTokens];
+    float sum[kTallTokens], scale[kTallTokens];
 };
 
 struct TallShape {
@@ -291,8 +291,9 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
     extern __shared__ uint8_t raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     const uint32_t right_bytes = (uint32_t)f.rows * 128, stage_bytes = kTallLeftBytes + right_bytes;
-    float* part = reinterpret_cast<float*>(ring + f.stages * stage_bytes);            // [token][rank]
-    TallShared& sh = *reinterpret_cast<TallShared*>(part + kTallTokens * a.rank);
+    float* part = reinterpret_cast<float*>(ring + f.stages * stage_bytes);            // [token][rank], an odd stride
+    const int stride = a.rank | 1;
+    TallShared& sh = *reinterpret_cast<TallShared*>(part + kTallTokens * stride);
     cg::cluster_group cluster = cg::this_cluster();
     const int crank = (int)cluster.block_rank(), cranks = (int)cluster.num_blocks();
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // (known to be the same for a whole warp)
@@ -315,7 +316,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
         tc_fence_before();
     }
     if (threadIdx.x < kTallTokens) sh.sum[threadIdx.x] = 0.0f;
-    for (int i = threadIdx.x; i < kTallTokens * a.rank; i += kTallThreads) part[i] = 0.0f;
+    for (int i = threadIdx.x; i < kTallTokens * stride; i += kTallThreads) part[i] = 0.0f;
     // ones: bf16 0x3F80, fp16 0x3C00
     for (int i = threadIdx.x; i < f.stages * f.lead * 8; i += kTallThreads) {
         const uint32_t one = BF16 ? 0x3F803F80u : 0x3C003C00u;
@@ -325,6 +326,10 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
     __syncthreads();
     tc_fence_after();
     find_adapters<kTallTokens>(a, t0, sh.ids);
+    if (threadIdx.x < kTallTokens) {
+        const int id = sh.ids[threadIdx.x];
+        sh.scale[threadIdx.x] = id < 0 ? 0.0f : a.scale ? a.scale[id] : 1.0f;
+    }
     if (warp == 0) {
         int mine[kTallTokens / 32], count = 0;
 #pragma unroll
@@ -430,7 +435,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
                         if (mine) {
 #pragma unroll
                             for (int k = 0; k < 8; ++k)
-                                if (r + k < a.rank) part[row * a.rank + r + k] = y[k];
+                                if (r + k < a.rank) part[row * stride + r + k] = y[k];
                         }
                     }
                 }
@@ -445,20 +450,30 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
         tc_free<false>(tmem, (uint32_t)f.columns);
     }
     cluster.sync();
-    // the cluster's sums: every CTA a block of the tokens, a thread a rank of one, then a thread a token
+    // The cluster's sums: every CTA a block of the tokens, a thread some ranks of one (what it needs of the others is on its way together), then
+    // a thread a token.
     const int most = kTallTokens / cranks, row0 = crank * most;
     if (f.slots > 0) {
-        for (int i = threadIdx.x; i < most * a.rank; i += kTallThreads) {
-            const int row = row0 + i / a.rank, id = sh.ids[row];
-            if (id == kNoRequest) continue;
-            float s = 0.0f;
-            if (id >= 0) {
-                for (int c = 0; c < cranks; ++c) s += cluster.map_shared_rank(part, c)[row0 * a.rank + i];
-                if (a.scale) s *= a.scale[id];
+        // (a lane a rank, four of a warp's rows at a time)
+        constexpr int N = 4, W = kTallThreads / 32;
+        for (int r = lane; r < a.rank; r += 32)
+            for (int first = row0 + warp; first < row0 + most; first += N * W) {
+                float s[N] = {};
+                for (int c = 0; c < cranks; ++c) {
+                    const float* p = cluster.map_shared_rank(part, c) + r;
+#pragma unroll
+                    for (int k = 0; k < N; ++k)
+                        if (first + k * W < row0 + most) s[k] += p[(first + k * W) * stride];
+                }
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const int row = first + k * W;
+                    if (row >= row0 + most || sh.ids[row] == kNoRequest) continue;
+                    const float y = s[k] * sh.scale[row];                             // (zero for tokens without an adapter)
+                    a.hidden[(t0 + row) * a.rank + r] = y;
+                    part[row * stride + r] = y;                                       // (no other CTA reads these)
+                }
             }
-            a.hidden[(t0 + row0) * a.rank + i] = s;
-            part[row0 * a.rank + i] = s;                                              // (no other CTA reads these)
-        }
         __syncthreads();
     }
     if ((int)threadIdx.x < most && t0 + row0 + (int)threadIdx.x < a.tokens) {
@@ -467,7 +482,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
         a.ids[t] = id;
         if (f.slots > 0) {
             float top = 0.0f;
-            for (int r = 0; r < a.rank; ++r) top = fmaxf(top, fabsf(part[row * a.rank + r]));
+            for (int r = 0; r < a.rank; ++r) top = fmaxf(top, fabsf(part[row * stride + r]));
             a.hidden_scale[t] = 1.0f / scale_to_range(id == kNoRequest ? 0.0f : top);
         }
         if (f.lead > 0) {
@@ -582,7 +597,7 @@ static int launch_tall(zipml_ctx* ctx, const ShrinkArgs& a, int dtype, bool sums
     }
     f.rows = (f.lead + f.slots * f.ranks8 + 15) / 16 * 16;
     f.columns = f.rows > 0 ? 512 : 32;
-    const size_t stage = kTallLeftBytes + (size_t)f.rows * 128, fixed = 1024 + sizeof(float) * kTallTokens * a.rank + sizeof(TallShared);
+    const size_t stage = kTallLeftBytes + (size_t)f.rows * 128, fixed = 1024 + sizeof(float) * kTallTokens * (a.rank | 1) + sizeof(TallShared);
     f.stages = (int)((200 * 1024 - fixed) / stage);
     if (f.stages > kTallMostStages) f.stages = kTallMostStages;
     const size_t smem = fixed + f.stages * stage;
