@@ -587,15 +587,20 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 uint8_t* tok = right + group * Shape::kRightBytes;
                 const auto store_hidden = [&](auto type, int from) {
                     using T = decltype(type);
+                    float inv[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const int u = from + gid + i * kGroupThreads;
+                        inv[i] = u < units ? 1.0f / sh.token[lo + (u >> row_shift)].hidden_scale : 0.0f;       // (a power of two)
+                    }
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         const int u = from + gid + i * kGroupThreads, t = lo + (u >> row_shift), chunk = u & ((1 << row_shift) - 1);
                         if (u >= units) continue;
-                        const float inv = 1.0f / sh.token[t].hidden_scale;         // (a power of two)
                         uint32_t high[4], low[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const float x = v[i][2 * k] * inv, y = v[i][2 * k + 1] * inv;
+                            const float x = v[i][2 * k] * inv[i], y = v[i][2 * k + 1] * inv[i];
                             high[k] = pack_pair<T>(x, y);
                             const float2 f = unpack_pair<T>(high[k]);
                             low[k] = pack_pair<T>(x - f.x, y - f.y);
@@ -646,28 +651,46 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 for (int c = group; c < NT / 16; c += kGroups, turn ^= 1) {
                     T* stage = stages + turn * 16 * kProjRows;            // (two buffers in turn: the next barrier tells that this one has been read)
                     tc_load_wait();
+                    // (four tokens' values before the first is stored: a store to shared memory holds back every load behind it)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const ProjToken tok = sh.token[c * 16 + i];
-                        float sum = __uint_as_float(v[i]);
-                        if constexpr (Shape::kIssuers == 2) sum += __uint_as_float(v2[i]);
-                        const float y = fmaf(alpha * tok.row_scale, sum, fmaf(tok.hidden_scale, __uint_as_float(w[i]), beta * tok.sum));
-                        if constexpr (MODE == 0) join[(c * 16 + i) * kProjRows] = y;
-                        else if constexpr (MODE == 1) stage[i * kProjRows + row] = from_float<T>(y);
-                        else if (tok.id != kNoRequest && feature < a.features) reinterpret_cast<T*>(a.out)[(t0 + c * 16 + i) * a.ldo + feature] = from_float<T>(y);
+                    for (int i0 = 0; i0 < 16; i0 += 4) {
+                        ProjToken tok[4];
+                        float y[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) tok[i] = sh.token[c * 16 + i0 + i];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float sum = __uint_as_float(v[i0 + i]);
+                            if constexpr (Shape::kIssuers == 2) sum += __uint_as_float(v2[i0 + i]);
+                            y[i] = fmaf(alpha * tok[i].row_scale, sum, fmaf(tok[i].hidden_scale, __uint_as_float(w[i0 + i]), beta * tok[i].sum));
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int t = i0 + i;
+                            if constexpr (MODE == 0) join[(c * 16 + t) * kProjRows] = y[i];
+                            else if constexpr (MODE == 1) stage[t * kProjRows + row] = from_float<T>(y[i]);
+                            else if (tok[i].id != kNoRequest && feature < a.features) reinterpret_cast<T*>(a.out)[(t0 + c * 16 + t) * a.ldo + feature] = from_float<T>(y[i]);
+                        }
                     }
                     if (c + kGroups < NT / 16) load(c + kGroups);         // (on its way while these rows go out)
                     if constexpr (MODE == 1) {
                         asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(kGroupThreads) : "memory");
+                        const int at = f0 + (gid & 15) * 8;
+                        uint4 y[2];
+                        bool there[2];
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            const int u = gid + i * kGroupThreads, t = c * 16 + (u >> 4), at = f0 + (u & 15) * 8;
-                            if (sh.token[t].id == kNoRequest || at >= a.features) continue;
-                            const uint4 y = *reinterpret_cast<const uint4*>(stage + (u >> 4) * kProjRows + (u & 15) * 8);
-                            uint16_t* p = reinterpret_cast<uint16_t*>(a.out) + (t0 + t) * a.ldo + at;
-                            if (at + 8 <= a.features) *reinterpret_cast<uint4*>(p) = y;
+                            const int t = (gid >> 4) + i * 8;
+                            y[i] = *reinterpret_cast<const uint4*>(stage + t * kProjRows + (gid & 15) * 8);
+                            there[i] = sh.token[c * 16 + t].id != kNoRequest && at < a.features;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            if (!there[i]) continue;
+                            uint16_t* p = reinterpret_cast<uint16_t*>(a.out) + (t0 + c * 16 + (gid >> 4) + i * 8) * a.ldo + at;
+                            if (at + 8 <= a.features) *reinterpret_cast<uint4*>(p) = y[i];
                             else {
-                                const uint32_t e[4] = {y.x, y.y, y.z, y.w};
+                                const uint32_t e[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
 #pragma unroll
                                 for (int k = 0; k < 8; ++k)
                                     if (at + k < a.features) p[k] = (uint16_t)(e[k >> 1] >> (16 * (k & 1)));
