@@ -197,19 +197,15 @@ __device__ __forceinline__ void unpack_stage(uint32_t (&w)[kUnits][4], uint8_t* 
     }
 }
 
-// Eight 16-bit values with what is not finite replaced by zero.  `lowest`: the exponent's lowest bit in both halves of a word; added to a value
-// without its sign it carries into the sign's place exactly where the exponent is all ones.
+// Marks (the sign's place) of what is not finite among 16-bit values, and the values with zero in its place.  `lowest`: the exponent's lowest bit in
+// both halves of a word; added to a value without its sign it carries into the sign's place exactly where the exponent is all ones.
 __device__ __forceinline__ uint32_t not_finite(uint32_t w, uint32_t lowest) { return ((w & 0x7fff7fffu) + lowest) & 0x80008000u; }
-__device__ __forceinline__ void keep_finite(uint4& w, uint32_t lowest, bool& bad) {
-    if ((not_finite(w.x, lowest) | not_finite(w.y, lowest) | not_finite(w.z, lowest) | not_finite(w.w, lowest)) == 0) return;
-    bad = true;
-    uint32_t* p = &w.x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t n = not_finite(p[i], lowest);
-        if (n & 0x8000u) p[i] &= 0xffff0000u;
-        if (n & 0x80000000u) p[i] &= 0x0000ffffu;
-    }
+__device__ __forceinline__ uint32_t not_finite(const uint4& w, uint32_t lowest) {
+    return not_finite(w.x, lowest) | not_finite(w.y, lowest) | not_finite(w.z, lowest) | not_finite(w.w, lowest);
+}
+__device__ __forceinline__ uint32_t keep_finite(uint32_t w, uint32_t lowest) {
+    const uint32_t n = not_finite(w, lowest);
+    return w & ~((n >> 15) * 0xffffu);                    // (a half's mark becomes all of its bits)
 }
 
 template <int NT, bool BACK, bool BF16, bool PAIR>
@@ -553,15 +549,20 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 static_assert(kGroupThreads == 8 * 16, "a unit of ranks a turn");
                 const int f = f0 + (gid & 15) * 8, there = min(max(a.features - f, 0), 8);
                 const uint16_t* column = up + f;
+                const uint16_t* from[U];
+                bool held[U];
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
                     const int at = j * kRankChunk + i * 8, e = (int)__umulhi((uint32_t)at, per_rank8), r = at - e * rank8 + (gid >> 4);
-                    w[i] = make_uint4(0, 0, 0, 0);
-                    if (e < entries && r < a.rank) {
-                        const uint16_t* p = column + ((int64_t)sh.entry_id[e] * a.rank + r) * a.features;
-                        if (wide && there == 8) w[i] = *reinterpret_cast<const uint4*>(p);
-                        else w[i] = load8_16(p, there, false);
-                    }
+                    held[i] = e < entries && r < a.rank;
+                    from[i] = column + ((int64_t)sh.entry_id[held[i] ? e : 0] * a.rank + r) * a.features;
+                }
+                if (wide && there == 8) {
+#pragma unroll
+                    for (int i = 0; i < U; ++i) w[i] = held[i] ? *reinterpret_cast<const uint4*>(from[i]) : make_uint4(0, 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < U; ++i) w[i] = load8_16(from[i], held[i] ? there : 0, false);
                 }
                 lo = PAIR ? side * Shape::kRightRows : sh.window_lo[j];
                 const int n = PAIR ? Shape::kRightRows : sh.window_n[j];
@@ -577,11 +578,19 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 uint8_t* dst = left + group * kLeftBytes;
+                uint32_t marks = 0;
+#pragma unroll
+                for (int i = 0; i < U; ++i) marks |= not_finite(w[i], lowest);
+                if (marks != 0) {
+                    bad = true;
+#pragma unroll
+                    for (int i = 0; i < U; ++i)
+                        w[i] = make_uint4(keep_finite(w[i].x, lowest), keep_finite(w[i].y, lowest), keep_finite(w[i].z, lowest), keep_finite(w[i].w, lowest));
+                }
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
                     const int u = gid + i * kGroupThreads, k = u >> 4, chunk = u & 15;
                     if (k >= padded) continue;
-                    keep_finite(w[i], lowest, bad);
                     *reinterpret_cast<uint4*>(dst + (chunk >> 3) * (kLeftBytes / 2) + k * 128 + (((chunk & 7) ^ (k & 7)) << 4)) = w[i];
                 }
                 uint8_t* tok = right + group * Shape::kRightBytes;
