@@ -29,8 +29,8 @@ namespace cg = cooperative_groups;
 //
 // What bounds it: shared memory.  A stage of a pair's CTA writes 16 KB of tokens and 4 or 8 KB of codes, reads those, writes 16 KB of left
 // operand, and the tensor cores read 32 KB: some 600 cycles at 128 bytes each, and it takes 560 to 590, where the product alone takes 512.  A
-// tile then waits for its start (2,000 cycles), the adapters (4,500) and the epilogue (9,000).  8192 x 8192 x 8192, 4 bits, rank 32: 800 us,
-// 1.37 PFLOP/s; 4096 tokens x 4096 x 16384, 8 bits, rank 16: 475 us; backward 8192 x 8192 x 8192, 8 bits: 860 us.  With single CTAs of 128
+// tile then waits for its start (2,000 cycles), the adapters (4,500) and the epilogue (7,500).  8192 x 8192 x 8192, 4 bits, rank 32: 776 us,
+// 1.43 PFLOP/s; 4096 tokens x 4096 x 16384, 8 bits, rank 16: 460 us; backward 8192 x 8192 x 8192, 8 bits: 840 us.  With single CTAs of 128
 // x 256, which read every token twice as often from L2, the first took 990 us.  Few tokens: 470 to 530 cycles a stage against the 130 that the
 // codes' bytes would take; without the unpacking 285.
 // ---------------------------------------------------------------------------------------------

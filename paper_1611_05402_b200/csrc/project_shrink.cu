@@ -497,13 +497,16 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
 // ---------------------------------------------------------------------------------------------
 // The backward pass's rows: sum z mid and the largest |z step| of a row, then z step 2^k in fp16 (11 bits where bf16 would keep 8, one
 // rounding).  A CTA takes several rows, so that the grids' 8 bytes a column are read once for all of them; the second look at z finds it in
-// L1 or L2.  Bound by HBM: z once in, once out.
+// L1 or L2.  Bound by HBM: z once in, once out.  Nothing here needs what the kernel before it, which takes the same tokens onto their
+// ranks, makes: it starts beside that one and ends after it, so that whoever waits for this kernel has waited for both.  (8192 x 8192:
+// one after the other 91 us, together 77.)
 // ---------------------------------------------------------------------------------------------
 constexpr int kScaleRows = 4;
 constexpr int kScaleThreads = 256;
 
 template <typename T>
-__global__ void __launch_bounds__(kScaleThreads) scale_rows_kernel(ShrinkArgs a) {
+__global__ void __launch_bounds__(kScaleThreads) scale_rows_kernel(ShrinkArgs a, int early) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ float sums[kScaleRows][kScaleThreads / 32], tops[kScaleRows][kScaleThreads / 32];
     const T* z = reinterpret_cast<const T*>(a.z);
     const int64_t t0 = (int64_t)blockIdx.x * kScaleRows;
@@ -576,6 +579,7 @@ __global__ void __launch_bounds__(kScaleThreads) scale_rows_kernel(ShrinkArgs a)
             *reinterpret_cast<uint4*>(a.scaled + (t0 + r) * a.ld_scaled + j) = make_uint4(o[0], o[1], o[2], o[3]);
         }
     }
+    if (early) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // Whether the kernel for many tokens takes them: rows that tensor copies can read, enough tokens to fill its tiles and few adapters in each.
@@ -631,10 +635,20 @@ static int launch_tall(zipml_ctx* ctx, const ShrinkArgs& a, int dtype, bool sums
 
 static int launch_scale_rows(zipml_ctx* ctx, const ShrinkArgs& a, int dtype) {
     const unsigned grid = (unsigned)((a.tokens + kScaleRows - 1) / kScaleRows);
-    if (dtype == ZIPML_BF16) scale_rows_kernel<__nv_bfloat16><<<grid, kScaleThreads, 0, ctx->stream>>>(a);
-    else scale_rows_kernel<__half><<<grid, kScaleThreads, 0, ctx->stream>>>(a);
+    const int early = capturing(ctx) ? 0 : 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kScaleThreads);
+    cfg.stream = ctx->stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = (unsigned)early;
+    const cudaError_t e = dtype == ZIPML_BF16 ? cudaLaunchKernelEx(&cfg, &scale_rows_kernel<__nv_bfloat16>, a, early)
+                                              : cudaLaunchKernelEx(&cfg, &scale_rows_kernel<__half>, a, early);
     ctx->launches += 1;
-    return cuda_status(cudaGetLastError());
+    return cuda_status(e != cudaSuccess ? e : cudaGetLastError());
 }
 
 template <typename T, bool BACK, int RT>
@@ -680,11 +694,8 @@ static int launch_shrink_ranks(zipml_ctx* ctx, const ShrinkArgs& a) {
 
 int launch_shrink(zipml_ctx* ctx, const ShrinkArgs& a, int dtype, bool backward) {
     if (tall_takes(a)) {
-        if (backward && a.scaled) {
-            const int rc = launch_scale_rows(ctx, a, dtype);
-            if (rc != ZIPML_OK) return rc;
-        }
-        return launch_tall(ctx, a, dtype, !backward);
+        const int rc = launch_tall(ctx, a, dtype, !backward);
+        return rc != ZIPML_OK || !backward || !a.scaled ? rc : launch_scale_rows(ctx, a, dtype);
     }
     if (dtype == ZIPML_BF16) return backward ? launch_shrink_ranks<__nv_bfloat16, true>(ctx, a) : launch_shrink_ranks<__nv_bfloat16, false>(ctx, a);
     return backward ? launch_shrink_ranks<__half, true>(ctx, a) : launch_shrink_ranks<__half, false>(ctx, a);
