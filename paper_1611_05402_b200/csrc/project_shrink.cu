@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
 // rounding).  A CTA takes several rows, so that the grids' 8 bytes a column are read once for all of them; the second look at z finds it in
 // L1 or L2.  Bound by HBM: z once in, once out.  Nothing here needs what the kernel before it, which takes the same tokens onto their
 // ranks, makes: it starts beside that one and ends after it, so that whoever waits for this kernel has waited for both.  (Whole
-// backward calls, one after the other and beside one another: 2048 x 4096 x 4096 152 and 147 us, 8192 x 8192 x 8192 1,137 and 1,126.)
+// backward calls, one after the other and beside one another: 2048 x 4096 x 4096 152 and 147 us, 8192 x 8192 x 8192 1,137 and 1,126: the longer one within its noise.)
 // ---------------------------------------------------------------------------------------------
 constexpr int kScaleRows = 4;
 constexpr int kScaleThreads = 256;
