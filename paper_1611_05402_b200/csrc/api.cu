@@ -819,7 +819,7 @@ int zipml_project_backward(zipml_ctx* ctx, const zipml_dataset* weights, const z
     float* v = nullptr;
     if (tokens > 0 && (dX || grad_a)) {
         const size_t bytes = 4 * carve_size(sizeof(float) * (size_t)tokens) + carve_size(sizeof(float) * (size_t)tokens * rank) +
-                             (dX ? carve_size(2 * (size_t)tokens * (size_t)ld_scaled) : 0);
+                             (dX ? carve_size(2 * 2 * (size_t)tokens * (size_t)ld_scaled) : 0);
         unsigned char* ws = nullptr;
         rc = project_reserve(ctx, bytes, &ws);
         if (rc != ZIPML_OK) return rc;
@@ -836,7 +836,7 @@ int zipml_project_backward(zipml_ctx* ctx, const zipml_dataset* weights, const z
             s.hidden = v = carve.take<float>((size_t)tokens * rank);
         }
         s.lo = weights->feat_lo; s.step = weights->feat_step; s.center = code_center(weights->bits);
-        if (dX) { s.scaled = reinterpret_cast<__half*>(carve.take<uint16_t>((size_t)tokens * (size_t)ld_scaled)); s.ld_scaled = ld_scaled; }
+        if (dX) { s.scaled = reinterpret_cast<__half*>(carve.take<uint16_t>(2 * (size_t)tokens * (size_t)ld_scaled)); s.ld_scaled = ld_scaled; }
         s.status = ctx->d_status;
         rc = launch_shrink(ctx, s, dtype, true);
         if (rc != ZIPML_OK) return rc;

@@ -19,7 +19,11 @@ namespace cg = cooperative_groups;
 //             visible to the tensor cores.  Forward: a code row is one depth and holds the features (MN-major operand);
 //             backward: a code row is a feature (K-major).
 //   tokens    A tensor copy lays the right operand out itself.  Of a pair each CTA brings half of it, and the tensor cores share it.
-//   product   One lane issues 128 (256) x NT x 16 four times, sums in tensor memory.
+//   product   One lane issues 128 (256) x NT x 16 four times, sums in tensor memory.  Backward: eight times, since dy step is not a 16-bit
+//             number: in one part it would be off by 2^-12, as much as the rounding of an fp16 result, and more wherever the codes'
+//             products and the lower ends' share cancel.  Its two parts (see split_scaled) have sums of their own.  The tensor cores cut what they
+//             add to a sum instead of rounding it, so one sum of 1,024 products over a depth of 8192 was 1.6e-5 of the result off; the
+//             high parts' sums are exact, and what the low ones' lose is that much of a part a few hundred times smaller.
 // The adapters then take further stages: the ranks of the tile's adapters, each padded to a multiple of 8, follow one another as a depth of
 // their own, 32 a stage.  up_i's rows are the left operand as they lie, hidden the right one, in two 16-bit parts (high and low: 16 or more
 // bits), zero for tokens of other adapters, over the 16-token windows that hold the stage's tokens.  Their sums have columns of their own,
@@ -30,8 +34,9 @@ namespace cg = cooperative_groups;
 // What bounds it: shared memory.  A stage of a pair's CTA writes 16 KB of tokens and 4 or 8 KB of codes, reads those, writes 16 KB of left
 // operand, and the tensor cores read 32 KB: some 600 cycles at 128 bytes each, and it takes 560 to 590, where the product alone takes 512.  A
 // tile then waits for its start (2,000 cycles), the adapters (4,500) and the epilogue (7,500).  8192 x 8192 x 8192, 4 bits, rank 32: 776 us,
-// 1.43 PFLOP/s; 4096 tokens x 4096 x 16384, 8 bits, rank 16: 460 us; backward 8192 x 8192 x 8192, 8 bits: 840 us.  With single CTAs of 128
-// x 256, which read every token twice as often from L2, the first took 990 us.  Few tokens: 470 to 530 cycles a stage against the 130 that the
+// 1.43 PFLOP/s; 4096 tokens x 4096 x 16384, 8 bits, rank 16: 460 us; backward 8192 x 8192 x 8192, 8 bits: 1,359 us, whose
+// two parts' products run at 1.62 PFLOP/s (840 us with one part of 11 bits).  With single CTAs of 128 x 256, which read every token twice as often
+// from L2, the first took 990 us.  Few tokens: 470 to 530 cycles a stage against the 130 that the
 // codes' bytes would take; without the unpacking 285.
 // ---------------------------------------------------------------------------------------------
 constexpr int kProjRows = 128;                // features of a CTA
@@ -52,20 +57,25 @@ constexpr uint32_t kLeftBytes = kProjRows * kProjDepth * 2;
 // cycles), in the left ring's order.  The groups' rings have a multiple of kGroups slots, so that a slot is always the same group's: a
 // barrier tells a phase from the one before it only, and a group that came to a slot whose last phase belonged to another could be a phase
 // early.
-template <int NT, bool PAIR>
+template <int NT, bool PAIR, bool BACK>
 struct ProjShape {
     static constexpr int kLeft = 2 * kGroups;
-    static constexpr int kRight = PAIR || NT == 128 ? 4 : 6;
+    static constexpr int kParts = BACK ? 2 : 1;                         // of the tokens' operand
+    static constexpr int kRight = BACK ? (NT >= 128 ? 3 : NT == 64 ? 4 : 6) : NT >= 128 ? 4 : 6;
     static constexpr int kRightRows = PAIR ? NT / 2 : NT;               // tokens of the operand that lie in this CTA
-    static constexpr uint32_t kRightBytes = kRightRows * kProjDepth * 2;
-    static constexpr uint32_t kCodeRing = (NT >= 128 ? 6 : NT == 64 ? 9 : 12) * kProjRows * kProjDepth;     // bytes for packed codes
+    static constexpr uint32_t kPartBytes = kRightRows * kProjDepth * 2, kRightBytes = kParts * kPartBytes;
+    static constexpr uint32_t kCodeRing = (NT >= 128 ? (BACK ? 3 : 6) : NT == 64 ? (BACK ? 6 : 9) : 12) * kProjRows * kProjDepth;     // bytes for packed codes
     static_assert(kRight >= kGroups && kRight <= kLeft && kLeft % kGroups == 0 && kMostSlots % kGroups == 0, "slots by group");
     static constexpr uint32_t kRing = kLeft * kLeftBytes + kRight * kRightBytes + kCodeRing;
-    // Tensor memory: the codes' sums of each issuing warp, then the adapters'.  Two warps issue where products are small: a turn's own
-    // instructions, one after the other, take some 400 cycles, the products of 64 tokens 130.
+    // Tensor memory: the codes' sums of each issuing warp, for each part, then the adapters'.  Two warps issue where products are small: a turn's own
+    // instructions, one after the other, take some 400 cycles, the products of 64 tokens 130 for each part.  Backward, the sums of 128
+    // tokens and of a pair fill tensor memory: the first issuer's low sums are added to its high ones before the adapters' take their place.
     static constexpr int kIssuers = PAIR ? 1 : 2;
-    static constexpr uint32_t kUpAt = kIssuers * NT;
-    static constexpr uint32_t kColumns = PAIR || NT == 128 ? 512 : NT == 64 ? 256 : 64;
+    static constexpr uint32_t kLowAt = kIssuers * NT;
+    static constexpr bool kMerge = BACK && NT >= 128;
+    static constexpr uint32_t kUpAt = kMerge ? kLowAt : kIssuers * kParts * NT;
+    static constexpr uint32_t kColumns = PAIR || NT == 128 ? 512 : BACK ? (NT == 64 ? 512 : 128) : NT == 64 ? 256 : 64;
+    static_assert(kUpAt + NT <= kColumns, "what was asked for");
     static constexpr int kWindows = PAIR ? 1 : 4 * NT;                   // stages of adapters at most, for their windows
 };
 
@@ -74,17 +84,18 @@ struct ProjToken {                            // what the epilogue needs of a to
     int id;
 };
 
-template <int NT, bool PAIR>
+template <int NT, bool PAIR, bool BACK>
 struct ProjShared {
+    using Shape = ProjShape<NT, PAIR, BACK>;
     ProjToken token[NT];
     uint64_t codes_full[kMostSlots], codes_empty[kMostSlots], written[2 * kGroups], full[2 * kGroups], empty[2 * kGroups];
-    uint64_t up_full[kGroups], up_empty[kGroups], codes_done, done, plan;
+    uint64_t up_full[kGroups], up_empty[kGroups], codes_done, merged, done, plan;
     uint32_t tmem;
     int gave_up;
     int entries;                              // adapters of this tile that fall to this CTA
-    int entry_id[NT], entry_lo[NT], entry_end[NT];
+    int entry_id[NT], entry_lo[PAIR ? 1 : NT], entry_end[PAIR ? 1 : NT];
     int entry[NT];                            // of a token, -1: none
-    uint16_t window_lo[ProjShape<NT, PAIR>::kWindows], window_n[ProjShape<NT, PAIR>::kWindows];
+    uint16_t window_lo[Shape::kWindows], window_n[Shape::kWindows];
 };
 
 // A slot of a ring and the parity of its current turn.
@@ -211,11 +222,11 @@ __device__ __forceinline__ uint32_t keep_finite(uint32_t w, uint32_t lowest) {
 template <int NT, bool BACK, bool BF16, bool PAIR>
 __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a, const __grid_constant__ CUtensorMap tokens_map,
                                                                   const __grid_constant__ CUtensorMap codes_map) {
-    using Shape = ProjShape<NT, PAIR>;
+    using Shape = ProjShape<NT, PAIR, BACK>;
     constexpr int L = Shape::kLeft, R = Shape::kRight;
     extern __shared__ uint8_t raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-    ProjShared<NT, PAIR>& sh = *reinterpret_cast<ProjShared<NT, PAIR>*>(ring + Shape::kRing);
+    ProjShared<NT, PAIR, BACK>& sh = *reinterpret_cast<ProjShared<NT, PAIR, BACK>*>(ring + Shape::kRing);
     uint8_t* const left = ring;
     uint8_t* const right = ring + L * kLeftBytes;
     uint8_t* const packed = right + R * Shape::kRightBytes;
@@ -251,6 +262,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             mbar_init(&sh.up_empty[i], 1);
         }
         mbar_init(&sh.codes_done, Shape::kIssuers);
+        mbar_init(&sh.merged, (PAIR ? 2 : 1) * kGroups * kGroupWarps);
         mbar_init(&sh.done, 1);
         mbar_init(&sh.plan, 32);
         sh.gave_up = 0;
@@ -283,10 +295,13 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 if constexpr (PAIR) {
                     // (both halves count on the first CTA's barrier; the other's bytes may come before they are expected)
                     if (side == 0) mbar_arrive_expect_tx(&sh.full[stage.slot], 2 * Shape::kRightBytes);
-                    tc_copy_2d_pair(dst, &tokens_map, (step0 + s) * kProjDepth, (int)t0 + side * Shape::kRightRows, tc_peer(&sh.full[stage.slot], 0));
+                    for (int p = 0; p < Shape::kParts; ++p)
+                        tc_copy_2d_pair(dst + p * Shape::kPartBytes, &tokens_map, (step0 + s) * kProjDepth, (int)(p * a.tokens + t0) + side * Shape::kRightRows,
+                                        tc_peer(&sh.full[stage.slot], 0));
                 } else {
                     mbar_arrive_expect_tx(&sh.full[stage.slot], Shape::kRightBytes);
-                    tc_copy_2d(dst, &tokens_map, (step0 + s) * kProjDepth, (int)t0, &sh.full[stage.slot]);
+                    for (int p = 0; p < Shape::kParts; ++p)
+                        tc_copy_2d(dst + p * Shape::kPartBytes, &tokens_map, (step0 + s) * kProjDepth, (int)(p * a.tokens + t0), &sh.full[stage.slot]);
                 }
             }
             __syncwarp();
@@ -359,8 +374,10 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             if (here) {
                 if (lane == 0) {
                     sh.entry_id[entries] = id;
-                    sh.entry_lo[entries] = first & ~15;
-                    sh.entry_end[entries] = (last + 16) & ~15;
+                    if constexpr (!PAIR) {
+                        sh.entry_lo[entries] = first & ~15;
+                        sh.entry_end[entries] = (last + 16) & ~15;
+                    }
                 }
                 ++entries;
             }
@@ -401,7 +418,10 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 const uint64_t lp = left_at + (uint32_t)la.slot * (kLeftBytes / 16), rp = right_at + (uint32_t)ra.slot * (Shape::kRightBytes / 16);
                 if (tc_elect()) {
 #pragma unroll
-                    for (int k = 0; k < kProjDepth / 16; ++k) tc_mma<PAIR>(sums, lp + k * (BACK ? 2 : 128), rp + k * 2, kind, s > issuer || k > 0);
+                    for (int p = 0; p < Shape::kParts; ++p)
+#pragma unroll
+                        for (int k = 0; k < kProjDepth / 16; ++k)
+                            tc_mma<PAIR>(sums + p * Shape::kLowAt, lp + k * (BACK ? 2 : 128), rp + p * (Shape::kPartBytes / 16) + k * 2, kind, s > issuer || k > 0);
                     tc_commit<PAIR>(&sh.empty[la.slot]);
                 }
                 __syncwarp();
@@ -413,7 +433,8 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 if (ok && rank8 > 0) {
                     const int count = up_stages(), total = sh.entries * rank8;
                     const uint64_t up_at = tc_operand(smem_u32(left), kLeftBytes / 2, 1024);
-                    for (int j = 0, slot = 0, turn = 0; j < count; ++j) {
+                    if (Shape::kMerge && count > 0) ok = __all_sync(0xffffffffu, tc_wait(&sh.merged, 0, gave_up, a.status, 113));
+                    for (int j = 0, slot = 0, turn = 0; ok && j < count; ++j) {
                         ok = __all_sync(0xffffffffu, tc_wait(&sh.up_full[slot], turn, gave_up, a.status, 98));
                         if (!ok) break;
                         tc_fence_after();
@@ -571,6 +592,29 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 load_hidden(j, 0);
             };
             if (group < count) load_stage(group);
+            if constexpr (Shape::kMerge) {
+                if (count > 0) ok = __all_sync(0xffffffffu, tc_wait(&sh.codes_done, 0, gave_up, a.status, 114));
+                if (count > 0 && ok) {
+                    tc_fence_after();
+                    const uint32_t lanes_at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+                    for (int c = group; c < NT / 16; c += kGroups) {
+                        uint32_t high[16], low[16];
+                        tc_load16(lanes_at + c * 16, high);
+                        tc_load16(lanes_at + Shape::kLowAt + c * 16, low);
+                        tc_load_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) high[i] = __float_as_uint(__uint_as_float(high[i]) + __uint_as_float(low[i]));
+                        tc_store16(lanes_at + c * 16, high);
+                    }
+                    tc_store_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (PAIR && side != 0) tc_arrive_at(tc_peer(&sh.merged, 0));
+                        else mbar_arrive(&sh.merged);
+                    }
+                }
+            }
             for (int j = group; ok && j < count; j += kGroups) {
                 const int padded = 8 << row_shift;
                 ok = j < kGroups ? tc_wait(&sh.codes_done, 0, gave_up, a.status, 102)
@@ -608,12 +652,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                         if (u >= units) continue;
                         uint32_t high[4], low[4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float x = v[i][2 * k] * inv[i], y = v[i][2 * k + 1] * inv[i];
-                            high[k] = pack_pair<T>(x, y);
-                            const float2 f = unpack_pair<T>(high[k]);
-                            low[k] = pack_pair<T>(x - f.x, y - f.y);
-                        }
+                        for (int k = 0; k < 4; ++k) split_pair<T>(v[i][2 * k] * inv[i], v[i][2 * k + 1] * inv[i], high[k], low[k]);
                         uint8_t* p = tok + (PAIR ? t - lo : t) * 128;
                         *reinterpret_cast<uint4*>(p + ((chunk ^ (t & 7)) << 4)) = make_uint4(high[0], high[1], high[2], high[3]);
                         *reinterpret_cast<uint4*>(p + (((chunk + 4) ^ (t & 7)) << 4)) = make_uint4(low[0], low[1], low[2], low[3]);
@@ -642,6 +681,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             const bool have_up = sh.entries > 0, wide_out = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * 2)) & 15) == 0;
             if (crank != 0) beta = 0.0f;
             const uint32_t lanes_at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+            const bool merged = Shape::kMerge && have_up;
             uint32_t v[16] = {}, v2[Shape::kIssuers == 2 ? 16 : 1] = {}, w[16] = {};
             const auto load = [&](int c) {
                 if (steps > 0) tc_load16(lanes_at + c * 16, v);
@@ -659,6 +699,22 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 if (group < NT / 16) load(group);
                 for (int c = group; c < NT / 16; c += kGroups, turn ^= 1) {
                     T* stage = stages + turn * 16 * kProjRows;            // (two buffers in turn: the next barrier tells that this one has been read)
+                    if constexpr (Shape::kParts == 2) {
+                        uint32_t low[16];
+                        if (steps > 0 && !merged) {
+                            tc_load16(lanes_at + Shape::kLowAt + c * 16, low);
+                            tc_load_wait();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(low[i]));
+                        }
+                        if constexpr (Shape::kIssuers == 2)
+                            if (steps > 1) {
+                                tc_load16(lanes_at + Shape::kLowAt + NT + c * 16, low);
+                                tc_load_wait();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) v2[i] = __float_as_uint(__uint_as_float(v2[i]) + __uint_as_float(low[i]));
+                            }
+                    }
                     tc_load_wait();
                     // (four tokens' values before the first is stored: a store to shared memory holds back every load behind it)
 #pragma unroll
@@ -771,8 +827,8 @@ int encode_map(zipml_ctx* ctx, CUtensorMapDataType type, const void* base, int64
 template <int NT, bool BACK, bool BF16, bool PAIR = false>
 static int launch_project_as(zipml_ctx* ctx, const ProjectArgs& a, const CUtensorMap& tokens_map, const CUtensorMap& codes_map, int ranks) {
     auto kernel = &project_kernel<NT, BACK, BF16, PAIR>;
-    const size_t smem = 1024 + ProjShape<NT, PAIR>::kRing + sizeof(ProjShared<NT, PAIR>);
-    static_assert(1024 + ProjShape<NT, PAIR>::kRing + sizeof(ProjShared<NT, PAIR>) <= kMostShared, "what a block may have");
+    constexpr size_t smem = 1024 + ProjShape<NT, PAIR, BACK>::kRing + sizeof(ProjShared<NT, PAIR, BACK>);
+    static_assert(smem <= kMostShared, "what a block may have");
     const int rc = allow_shared(ctx, reinterpret_cast<const void*>(kernel), smem);
     if (rc != ZIPML_OK) return rc;
     constexpr int kTileRows = PAIR ? 2 * kProjRows : kProjRows;
@@ -797,11 +853,11 @@ static int launch_project_as(zipml_ctx* ctx, const ProjectArgs& a, const CUtenso
 }
 
 // Tokens of a tile and CTAs that divide the depth, by the cycles that the waves of tiles should take, as measured: 480 a stage and 1 for every
-// token of a single CTA's tile, 580 for a pair's, and for a tile's start, adapters and epilogue 4,500 and 42 for every token, where the
-// depth is divided 1,500 more.  (Whole calls: 64 tokens x 4096 x 14336
+// token of a single CTA's tile, 580 for a pair's (backward, with two parts: 540 and 3, 1,060), and for a tile's start, adapters and
+// epilogue 4,500 and 42 for every token, where the depth is divided 1,500 more.  (Whole calls: 64 tokens x 4096 x 14336
 // 44 us with tiles of 64, 45 with 128, 98 with 16; 200 x 4096 x 4096 33 us with the depth divided, 38 without; 1000 x 4096 x 4096
 // 51 us by pairs, 68 with tiles of 128, 96 with 64.)
-static void project_shape(const zipml_ctx* ctx, const ProjectArgs& a, int* tokens, int* ranks, bool* pair) {
+static void project_shape(const zipml_ctx* ctx, const ProjectArgs& a, bool backward, int* tokens, int* ranks, bool* pair) {
     const int64_t feature_tiles = (a.features + kProjRows - 1) / kProjRows, steps = (a.depth + kProjDepth - 1) / kProjDepth;
     double best = 0.0;
     for (const int nt : {16, 64, 128, 256})
@@ -810,7 +866,8 @@ static void project_shape(const zipml_ctx* ctx, const ProjectArgs& a, int* token
             if (nt == 256 && a.up && a.tokens < (int64_t)a.requests * 32) break;      // (a pair takes all of a tile's columns for each adapter)
             const int64_t ctas = (a.tokens + nt - 1) / nt * feature_tiles * r;
             const int64_t waves = (ctas + ctx->sm_count - 1) / ctx->sm_count;
-            const double cycles = (double)waves * ((double)((steps + r - 1) / r) * (nt == 256 ? 580 : 480 + nt) + 4500 + nt * 42 + (r > 1 ? 1500 : 0));
+            const int stage = backward ? (nt == 256 ? 1060 : 540 + 3 * nt) : nt == 256 ? 580 : 480 + nt;
+            const double cycles = (double)waves * ((double)((steps + r - 1) / r) * stage + 4500 + nt * 42 + (r > 1 ? 1500 : 0));
             if (best == 0.0 || cycles < best) { best = cycles; *tokens = nt; *ranks = r; }
         }
     *pair = *tokens == 256;
@@ -827,9 +884,10 @@ static int launch_project_typed(zipml_ctx* ctx, const ProjectArgs& a, const CUte
 int launch_project(zipml_ctx* ctx, const ProjectArgs& a, const void* tokens_operand, int64_t ld_operand, bool operand_bf16, const zipml_dataset* w, bool backward) {
     int nt = 16, ranks = 1;
     bool pair = false;
-    project_shape(ctx, a, &nt, &ranks, &pair);
+    project_shape(ctx, a, backward, &nt, &ranks, &pair);
     CUtensorMap tokens_map, codes_map;
-    int rc = encode_map(ctx, operand_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, tokens_operand, a.depth, a.tokens, ld_operand * 2,
+    int rc = encode_map(ctx, operand_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, tokens_operand, a.depth,
+                        (backward ? 2 : 1) * a.tokens, ld_operand * 2,
                         kProjDepth, pair ? nt / 2 : nt, CU_TENSOR_MAP_SWIZZLE_128B, &tokens_map);
     if (rc != ZIPML_OK) return rc;
     rc = encode_map(ctx, CU_TENSOR_MAP_DATA_TYPE_UINT8, w->plane1, w->row_bytes, w->m, w->row_bytes, (backward ? kProjDepth : kProjRows) * container_bits(a.bits) / 8,

@@ -42,6 +42,12 @@ template <> __device__ __forceinline__ uint32_t pack_pair<__half>(float a, float
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+// Two values as the sum of two pairs, the rounded values and the rounded rest of them: twice the type's bits.
+template <typename T> __device__ __forceinline__ void split_pair(float a, float b, uint32_t& high, uint32_t& low) {
+    high = pack_pair<T>(a, b);
+    const float2 f = unpack_pair<T>(high);
+    low = pack_pair<T>(a - f.x, b - f.y);
+}
 
 // Eight 16-bit values from p on, the first `count` of them (0 .. 8) there, the rest zero.  `wide`: p is 16-byte aligned.
 __device__ __forceinline__ uint4 load8_16(const void* p, int count, bool wide) {
@@ -54,6 +60,15 @@ __device__ __forceinline__ uint4 load8_16(const void* p, int count, bool wide) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// The same for a number of a row that scale_to_range has scaled: the high part a multiple of 2^5, 9 bits, the low one the rest in fp16's 11.  Codes
+// have 8 bits, so the high parts' products are multiples of 2^5 below 2^21, and fp32 holds their sums exactly up to 2^29.
+__device__ __forceinline__ void split_scaled(float a, float b, uint32_t& high, uint32_t& low) {
+    constexpr float kMagic = 1.5f * (float)(1 << 28);                     // (numbers around it are 2^5 apart)
+    const float x = __fsub_rn(__fadd_rn(a, kMagic), kMagic), y = __fsub_rn(__fadd_rn(b, kMagic), kMagic);
+    high = pack_pair<__half>(x, y);
+    low = pack_pair<__half>(a - x, b - y);
+}
+
 // Power of two that brings a value of magnitude `top` into [2^13, 2^14); 1 for zero and what is not finite.
 __device__ __forceinline__ float scale_to_range(float top) {
     if (!(top > 0.0f) || !(top <= 3.402823466e38f)) return 1.0f;
@@ -64,7 +79,8 @@ __device__ __forceinline__ float scale_to_range(float top) {
 // Stage 1, over tokens x `columns` values z (the forward pass's inputs, the backward pass's output gradients):
 //   hidden[t] = scale_i * (D_i z_t)   D_i: rank x columns, the adapter of token t
 //   forward:  sum[t] = sum_j z_tj
-//   backward: sum[t] = sum_j z_tj (lo_j + center step_j), scaled[t][j] = z_tj step_j * 2^k with 2^-k in row_scale[t]
+//   backward: sum[t] = sum_j z_tj (lo_j + center step_j), scaled[t][j] + scaled[tokens + t][j] = z_tj step_j * 2^k with 2^-k in row_scale[t],
+//             as split_scaled makes them
 struct ShrinkArgs {
     const void* z;
     int64_t tokens, ldz;
@@ -78,7 +94,7 @@ struct ShrinkArgs {
     float *sum, *row_scale, *hidden_scale;
     const float *lo, *step;      // backward
     float center;
-    __half* scaled;              // backward: tokens x ld_scaled
+    __half* scaled;              // backward: 2 tokens x ld_scaled, the products' high parts and then their low ones
     int64_t ld_scaled;
     void* copy;                  // forward: z once more in rows that tensor copies can take, or null
     int64_t ld_copy;

@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(32 * kShrinkWarps) shrink_kernel(ShrinkArgs a)
     }
     if constexpr (BACK) {
         if (slice == 0 && a.scaled) {
-            // z step, scaled by a power of two of the row so that fp16's range holds it: fp16 keeps 11 bits where bf16 would keep 8, one rounding
+            // z step, scaled by a power of two of the row so that fp16's range holds it, in two parts
             if (threadIdx.x < kShrinkRows) {
                 float m = 0.0f;
                 for (int c = 0; c < ranks; ++c) m = fmaxf(m, cluster.map_shared_rank(sh.cta_top, c)[threadIdx.x]);
@@ -237,16 +237,22 @@ __global__ void __launch_bounds__(32 * kShrinkWarps) shrink_kernel(ShrinkArgs a)
                 const uint4 x0 = use_g ? load8_16(zg + j, count, wide_z) : make_uint4(0, 0, 0, 0);
                 const uint4 x1 = use_h ? load8_16(zh + j, count, wide_z) : make_uint4(0, 0, 0, 0);
                 const uint32_t w0[4] = {x0.x, x0.y, x0.z, x0.w}, w1[4] = {x1.x, x1.y, x1.z, x1.w};
-                uint32_t o0[4], o1[4];
+                uint32_t high0[4], low0[4], high1[4], low1[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float2 f0 = unpack_pair<T>(w0[i]), f1 = unpack_pair<T>(w1[i]);
                     const float e0 = 2 * i < count ? a.step[j + 2 * i] : 0.0f, e1 = 2 * i + 1 < count ? a.step[j + 2 * i + 1] : 0.0f;
-                    o0[i] = pack_pair<__half>(f0.x * e0 * s0, f0.y * e1 * s0);
-                    o1[i] = pack_pair<__half>(f1.x * e0 * s1, f1.y * e1 * s1);
+                    split_scaled(f0.x * e0 * s0, f0.y * e1 * s0, high0[i], low0[i]);
+                    split_scaled(f1.x * e0 * s1, f1.y * e1 * s1, high1[i], low1[i]);
                 }
-                if (tg < a.tokens) *reinterpret_cast<uint4*>(a.scaled + tg * a.ld_scaled + j) = make_uint4(o0[0], o0[1], o0[2], o0[3]);
-                if (th < a.tokens) *reinterpret_cast<uint4*>(a.scaled + th * a.ld_scaled + j) = make_uint4(o1[0], o1[1], o1[2], o1[3]);
+                if (tg < a.tokens) {
+                    *reinterpret_cast<uint4*>(a.scaled + tg * a.ld_scaled + j) = make_uint4(high0[0], high0[1], high0[2], high0[3]);
+                    *reinterpret_cast<uint4*>(a.scaled + (a.tokens + tg) * a.ld_scaled + j) = make_uint4(low0[0], low0[1], low0[2], low0[3]);
+                }
+                if (th < a.tokens) {
+                    *reinterpret_cast<uint4*>(a.scaled + th * a.ld_scaled + j) = make_uint4(high1[0], high1[1], high1[2], high1[3]);
+                    *reinterpret_cast<uint4*>(a.scaled + (a.tokens + th) * a.ld_scaled + j) = make_uint4(low1[0], low1[1], low1[2], low1[3]);
+                }
             }
         }
     }
@@ -495,11 +501,10 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
 }
 
 // ---------------------------------------------------------------------------------------------
-// The backward pass's rows: sum z mid and the largest |z step| of a row, then z step 2^k in fp16 (11 bits where bf16 would keep 8, one
-// rounding).  A CTA takes several rows, so that the grids' 8 bytes a column are read once for all of them; the second look at z finds it in
-// L1 or L2.  Bound by HBM: z once in, once out.  Nothing here needs what the kernel before it, which takes the same tokens onto their
-// ranks, makes: it starts beside that one and ends after it, so that whoever waits for this kernel has waited for both.  (Whole
-// backward calls, one after the other and beside one another: 2048 x 4096 x 4096 152 and 147 us, 8192 x 8192 x 8192 1,137 and 1,126: the longer one within its noise.)
+// The backward pass's rows: sum z mid and the largest |z step| of a row, then z step 2^k in two parts (see split_scaled).  A CTA takes several
+// rows, so that the grids' 8 bytes a column are read once for all of them; the second look at z finds it in L1 or L2.  Bound by HBM: z once
+// in, twice out.  Nothing here needs what the kernel before it, which takes the same tokens onto their ranks, makes: it starts beside that
+// one and ends after it, so that whoever waits for this kernel has waited for both.
 // ---------------------------------------------------------------------------------------------
 constexpr int kScaleRows = 4;
 constexpr int kScaleThreads = 256;
@@ -570,13 +575,14 @@ __global__ void __launch_bounds__(kScaleThreads) scale_rows_kernel(ShrinkArgs a,
             if (t0 + r >= a.tokens) break;
             const uint4 w = load8_16(z + (t0 + r) * a.ldz + j, count, wide);
             const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-            uint32_t o[4];
+            uint32_t high[4], low[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float2 v = unpack_pair<T>(u[i]);
-                o[i] = pack_pair<__half>(v.x * step[2 * i] * scale[r], v.y * step[2 * i + 1] * scale[r]);
+                split_scaled(v.x * step[2 * i] * scale[r], v.y * step[2 * i + 1] * scale[r], high[i], low[i]);
             }
-            *reinterpret_cast<uint4*>(a.scaled + (t0 + r) * a.ld_scaled + j) = make_uint4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<uint4*>(a.scaled + (t0 + r) * a.ld_scaled + j) = make_uint4(high[0], high[1], high[2], high[3]);
+            *reinterpret_cast<uint4*>(a.scaled + (a.tokens + t0 + r) * a.ld_scaled + j) = make_uint4(low[0], low[1], low[2], low[3]);
         }
     }
     if (early) asm volatile("griddepcontrol.wait;" ::: "memory");

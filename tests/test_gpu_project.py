@@ -635,6 +635,66 @@ def test_offsets_past_32_bits(ctx):
     assert torch.equal(back[-2:].float(), (lo + st * codes).float().to(BF16).float())
 
 
+# --- how many bits results hold ---------------------------------------------------------------------------------------------------
+
+def beyond_rounding(got, want):
+    """How far `got` is from the value rounded to its type, relative to the whole."""
+    return ((got.double() - want.to(got.dtype).double()).norm() / want.norm()).item()
+
+
+def rounded_elsewhere(dtype, delta):
+    """What that comes to for values that were off by `delta` of the whole before they were rounded: one goes the other way, by a step u (eps of it at
+    most), with probability |d| / u, so the squares' sum is sum |d| u <= eps |d| |y|."""
+    return math.sqrt(delta * torch.finfo(dtype).eps) + delta
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("tokens,inputs,outputs,bits", [(1, 1000, 1000, 8), (33, 1000, 1000, 4), (100, 600, 1200, 8), (600, 520, 700, 4), (1500, 2304, 2304, 8), (2100, 1024, 8192, 8),
+                                                        (100, 1024, 8192, 4)])
+def test_results_are_rounded_once(ctx, tokens, inputs, outputs, bits, dtype):
+    """Nothing before the last rounding shows in a result: 2^-17 of it leaves room for sums in fp32 and for the 16 bits that two parts of bf16 hold."""
+    p = Problem(ctx, tokens, inputs, outputs, bits, dtype, 16, 2, [tokens], which=[1])
+    hidden = torch.zeros(tokens, 16, device=ctx.device)
+    kw = dict(adapters=p.adapters, starts=p.starts, which=p.which)
+    y = ctx.zipml_project(p.weights, p.x, hidden=hidden, **kw)
+    cp = ctx.zipml_checkpoint_encode(p.x, group=64)
+    dx, _, _ = ctx.zipml_project_backward(p.weights, p.dy, hidden=hidden, checkpoint=cp, **kw)
+    ctx.zipml_sync()
+    assert beyond_rounding(y, p.forward()[0]) <= rounded_elsewhere(dtype, 2.0**-17)
+    assert beyond_rounding(dx, p.backward(hidden, cp)[0]) <= rounded_elsewhere(dtype, 2.0**-17)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("tokens,inputs,outputs", [(3, 512, 384), (48, 384, 512), (400, 384, 512), (1400, 2304, 2304)])
+def test_results_where_the_codes_and_the_lower_ends_cancel(ctx, tokens, inputs, outputs, dtype):
+    """Every code the same and the lower ends such that they stand for about zero: what is left is the adapters' term, some 50 times smaller than either."""
+    p = Problem(ctx, tokens, inputs, outputs, 8, dtype, 16, 2, [tokens], which=[0], scale=False)
+    p.weights.plane1.fill_(200)
+    step = 1 + torch.rand(outputs, generator=torch.Generator().manual_seed(3)).to(ctx.device)
+    hidden = torch.zeros(tokens, 16, device=ctx.device)
+    kw = dict(adapters=p.adapters, starts=p.starts, which=p.which)
+    # (p's values are random with variance one, hidden and v about as large, a's 1 / inputs, b's 1 / 16)
+    for at, size in (("y", 50 / (72 * math.sqrt(inputs))), ("dx", 50 * math.sqrt(outputs / inputs) / (72 * math.sqrt(outputs)))):
+        p.weights.feat_step.copy_(step * size)
+        p.weights.feat_lo.copy_(-200 * p.weights.feat_step.double())
+        if at == "y":
+            got, want = ctx.zipml_project(p.weights, p.x, hidden=hidden, **kw), p.forward()[0]
+        else:
+            cp = ctx.zipml_checkpoint_encode(p.x, group=64)
+            got = ctx.zipml_project_backward(p.weights, p.dy, hidden=hidden, checkpoint=cp, **kw)[0]
+            want = p.backward(hidden, cp)[0]
+        ctx.zipml_sync()
+        parts = 72 * math.sqrt(inputs if at == "y" else outputs) * (step * size).norm() / math.sqrt(outputs) * math.sqrt(want.numel()) / want.norm()
+        assert 20 < parts < 200
+        # Tensor cores add sixteen products at a time to a sum S of fp32 and cut the result towards zero: each time up to a step, 2^-23 of |S|, is
+        # lost, always in S's direction, so y's k additions lose up to k 2^-23 |S|.  dx: what the low parts lose, 2^-12 of them; they are
+        # below 2^-9 of a row's largest value, that below 2^2.5 of the values' norm.  And the adapters' own 2^-16.
+        lost = (inputs / 16 + 2) * 2.0**-23 if at == "y" else 2.0**-18
+        assert beyond_rounding(got, want) <= rounded_elsewhere(dtype, 2.0**-16 + parts.item() * lost)
+
+
 # --- how calls are made -----------------------------------------------------------------------------------------------------------
 
 @gpu
