@@ -236,7 +236,9 @@ const char* zipml_last_kernel(const zipml_ctx* ctx);
 int zipml_barrier_latency(zipml_ctx* ctx, int32_t ctas, int32_t floats_per_cta, int32_t iterations, uint64_t* ns_out);
 /* Diagnostics for the error path of the device-side waits: one thread polls a flag that nothing sets, with
  * the engines' bounded-wait pattern and a limit of spin_limit polls (1 .. 2^24), gives up and records
- * ZIPML_ERR_TIMEOUT, which the next zipml_sync returns (and clears); the context stays usable.  The paper
+ * ZIPML_ERR_TIMEOUT, which the next zipml_sync returns (and clears); the context stays usable.  Then the same
+ * for the waits of zipml_project: in a block of four warps one waits spin_limit nanoseconds for what does not come, the
+ * others' waits are over at once, and all leave together.  The paper
  * has no counterpart; it exists so that the time-out route can be exercised without a hung kernel. */
 int zipml_wait_probe(zipml_ctx* ctx, int64_t spin_limit);
 /* Smallest legal row stride for n features: ceil(n*cb/8) rounded up to 16; 0 if bits is unsupported. */

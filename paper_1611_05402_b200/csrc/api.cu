@@ -632,7 +632,8 @@ int zipml_wait_probe(zipml_ctx* ctx, int64_t spin_limit) {
     if (e != cudaSuccess) return cuda_status(e);
     wait_probe_kernel<<<1, 32, 0, ctx->stream>>>(reinterpret_cast<const unsigned*>(ctx->ws), spin_limit, ctx->d_status);
     ctx->launches += 1;
-    return cuda_status(cudaGetLastError());
+    rc = cuda_status(cudaGetLastError());
+    return rc != ZIPML_OK ? rc : launch_group_probe(ctx, spin_limit);
 }
 
 int zipml_loss(zipml_ctx* ctx, int32_t mode, const float* A, int64_t m, int64_t n, int64_t lda,

@@ -306,10 +306,6 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             }
             __syncwarp();
         }
-        if (s < steps && lane == 0)                                        // (its stages' barriers want the unpacking warps too: they are waited for a while)
-            for (int i = max(0, s - R); i < s; ++i)
-                if (side == 0) tc_drain(&sh.full[i % L], (i / L) & 1);
-        __syncwarp();
     } else if (warp == 2) {
         // the packed codes
         int s = 0;
@@ -325,9 +321,6 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             }
             __syncwarp();
         }
-        if (s < steps && lane == 0)
-            for (int i = max(0, s - code_slots); i < s; ++i) tc_drain(&sh.codes_full[i % code_slots], (i / code_slots) & 1);
-        __syncwarp();
     } else if (warp == 3) {
         // what the first stage has found out about the tokens, and the adapters they need: each with the window of its tokens
         if (a.early) asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -455,8 +448,6 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
                 if (tc_elect()) tc_commit<PAIR>(&sh.done);
                 __syncwarp();
             }
-            if (!ok && lane == 0) tc_drain(issuer == 0 ? &sh.done : &sh.codes_done, 0);
-            __syncwarp();
         }
     } else if (warp >= kFirstPublisher && warp < kSecondIssuer) {
         // A group's stores, made visible to the tensor cores by a warp that has nothing else to do: the fence waits for what is on its way to
@@ -674,7 +665,8 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
             if (bad) set_status(a.status, ZIPML_ERR_NONFINITE, 103);
         }
         if (ok) ok = __all_sync(0xffffffffu, tc_wait(&sh.codes_done, 0, gave_up, a.status, 109) && tc_wait(&sh.done, 0, gave_up, a.status, 104));
-        if (ok) {
+        // (a group's warps meet at barriers of their own from here on: all of them or none)
+        if (tc_agree(ok, 1 + group, kGroupThreads)) {
             tc_fence_after();
             // The groups take every third 16 tokens.  A whole tile's rows pass through shared memory on their way out, so that a thread stores 16
             // bytes of a token's row; rows that are not aligned for that go out as they lie, 32 features a warp.
@@ -775,6 +767,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
         }
     }
     __syncthreads();
+    if (*gave_up) tc_settle();
     if constexpr (PAIR) cluster.sync();                               // (neither's memory goes while the other may still be at it)
     if (warp == 3) {
         tc_fence_after();
@@ -801,6 +794,32 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
         }
         cluster.sync();
     }
+}
+
+// How a group of project_kernel ends when one of its warps waits for what does not come: 128 threads, a barrier that nothing arrives at and
+// one that all has arrived at.  See zipml_wait_probe.
+__global__ void __launch_bounds__(kGroupThreads) group_probe_kernel(unsigned long long limit, DeviceStatus* status) {
+    __shared__ uint64_t never, there;
+    __shared__ int given_up;
+    volatile int* gave_up = &given_up;
+    if (threadIdx.x == 0) {
+        mbar_init(&never, 1);
+        mbar_init(&there, 1);
+        given_up = 0;
+        mbar_fence_init();
+        mbar_arrive(&there);
+    }
+    __syncthreads();
+    const bool ok = __all_sync(0xffffffffu, tc_wait(threadIdx.x < 32 ? &never : &there, 0, gave_up, status, 115, limit));
+    if (tc_agree(ok, 1, kGroupThreads)) asm volatile("bar.sync 1, %0;" ::"n"(kGroupThreads) : "memory");
+    __syncthreads();
+    if (*gave_up) tc_settle();
+}
+
+int launch_group_probe(zipml_ctx* ctx, int64_t limit_ns) {
+    group_probe_kernel<<<1, kGroupThreads, 0, ctx->stream>>>((unsigned long long)limit_ns, ctx->d_status);
+    ctx->launches += 1;
+    return cuda_status(cudaGetLastError());
 }
 
 int encode_map(zipml_ctx* ctx, CUtensorMapDataType type, const void* base, int64_t inner, int64_t rows, int64_t stride_bytes, int box_inner, int box_rows,

@@ -146,6 +146,7 @@ int launch_shrink(zipml_ctx* ctx, const ShrinkArgs& a, int dtype, bool backward)
 int launch_project(zipml_ctx* ctx, const ProjectArgs& a, const void* tokens_operand, int64_t ld_operand, bool operand_bf16, const zipml_dataset* w,
                    bool backward);
 int launch_project_grad(zipml_ctx* ctx, const GradArgs& a);
+int launch_group_probe(zipml_ctx* ctx, int64_t limit_ns);
 int launch_checkpoint_encode(zipml_ctx* ctx, const void* X, int dtype, int64_t m, int64_t n, int64_t ldx, uint64_t seed, const zipml_checkpoint* out);
 int launch_checkpoint_decode(zipml_ctx* ctx, const zipml_checkpoint* cp, int dtype, void* X, int64_t ldx);
 

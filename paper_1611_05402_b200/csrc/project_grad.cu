@@ -103,6 +103,7 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* 
     float base[MT][2] = {};
     const int others = ranks * kGradWarps, me = crank * kGradWarps + warp; // (a power of two of warps take the chunks in turn)
     bool any = false;                                      // has this adapter tokens?
+    bool lost = false;                                     // a copy of this warp's has not come: no further ones
     int turn = 0;                                          // chunks of the batches so far, of all warps
     uint32_t taken = 0, issued = 0;                        // of this one
     for (int first = 0; first < a.requests; first += kGradBatch) {
@@ -140,7 +141,7 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* 
         const auto step = [&](Cursor& at) { ++at.c; ++at.turn; settle(at); };
         Cursor ahead{0, 0, turn};
         const auto issue = [&] {                           // (into the slot that was read longest ago, by this warp)
-            if (ahead.i >= segments) return;
+            if (lost || ahead.i >= segments) return;
             const uint32_t slot = issued % SLOTS;
             if (tc_elect()) {
                 mbar_arrive_expect_tx(&sh.full[warp][slot], kGradSlotBytes);
@@ -180,7 +181,8 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* 
             const int t0 = sh.begin[at.i] + at.c * kGradChunk, e = sh.end[at.i];
             step(at);
             const uint32_t slot = taken % SLOTS;
-            if (copied && !__all_sync(0xffffffffu, tc_wait(&sh.full[warp][slot], (taken / SLOTS) & 1, gave_up, a.status, 108))) break;
+            lost = lost || (copied && !__all_sync(0xffffffffu, tc_wait(&sh.full[warp][slot], (taken / SLOTS) & 1, gave_up, a.status, 108)));
+            if (lost) break;
 #pragma unroll 1
             for (int tt = 0; tt < kGradChunk && t0 + tt < e; tt += 8) {
                 const Left l = next;
@@ -258,8 +260,6 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* 
         }
         turn = at.turn;
     }
-    if (*gave_up && lane == 0)                             // (copies that nobody has waited for)
-        for (; taken < issued; ++taken) tc_drain(&sh.full[warp][taken % SLOTS], (taken / SLOTS) & 1);
     if constexpr (RIGHT == kCodes) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -288,6 +288,7 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* 
     float* sums = reinterpret_cast<float*>(ring);
     const auto place = [](int r, int col) { return r * C + (((col >> 2) ^ ((col >> (CODES ? 5 : 4)) & 3) ^ ((r & 1) << 2)) << 2) + (col & 3); };
     __syncthreads();                                       // (the slots have been read)
+    if (*gave_up) tc_settle();
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll

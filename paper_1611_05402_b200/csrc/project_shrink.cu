@@ -378,9 +378,6 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
                 __syncwarp();
             }
         }
-        if (!ok && lane == 0)
-            for (int i = max(0, n - f.stages); i < n; ++i) tc_drain(&sh.full[i % f.stages], (i / f.stages) & 1);
-        __syncwarp();
     } else if (warp == 1) {
         int n = 0;
         bool ok = true;
@@ -451,6 +448,7 @@ __global__ void __launch_bounds__(kTallThreads, 1) shrink_tall_kernel(ShrinkArgs
         }
     }
     __syncthreads();
+    if (*gave_up) tc_settle();
     if (warp == 2) {
         tc_fence_after();
         tc_free<false>(tmem, (uint32_t)f.columns);

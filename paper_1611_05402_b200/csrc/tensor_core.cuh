@@ -6,6 +6,7 @@
 namespace zipml {
 
 constexpr unsigned long long kTcWaitNs = 2000000000ull;       // a wait that takes longer gives up
+constexpr unsigned long long kTcSettleNs = 20000000ull;
 
 __device__ __forceinline__ unsigned long long global_ns() {
     unsigned long long t;
@@ -13,28 +14,37 @@ __device__ __forceinline__ unsigned long long global_ns() {
     return t;
 }
 
-// Waits for a phase of a shared-memory barrier; false, with ZIPML_ERR_TIMEOUT recorded, after kTcWaitNs, or once another thread
-// of the block has given up.
-static __device__ __noinline__ bool tc_wait_long(uint64_t* bar, uint32_t parity, volatile int* gave_up, DeviceStatus* status, int where) {
+// Waits for a phase of a shared-memory barrier; false, with ZIPML_ERR_TIMEOUT recorded, after `limit`, or once another thread
+// of the block has given up.  Two warps that wait for the same thing may get different answers, if one gives up just before it comes: what they
+// do together afterwards (a barrier that wants all of them) needs tc_agree first.
+static __device__ __noinline__ bool tc_wait_long(uint64_t* bar, uint32_t parity, volatile int* gave_up, DeviceStatus* status, int where, unsigned long long limit) {
     const unsigned long long began = global_ns();
     for (;;) {
 #pragma unroll 1
         for (int i = 0; i < 64; ++i)
             if (mbar_try_wait(bar, parity)) return true;
         if (*gave_up) return false;
-        if (global_ns() - began > kTcWaitNs) break;
+        if (global_ns() - began > limit) break;
     }
     *gave_up = 1;
     set_status(status, ZIPML_ERR_TIMEOUT, where);
     return false;
 }
-__device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, volatile int* gave_up, DeviceStatus* status, int where) {
-    return mbar_try_wait(bar, parity) || tc_wait_long(bar, parity, gave_up, status, where);
+__device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, volatile int* gave_up, DeviceStatus* status, int where,
+                                        unsigned long long limit = kTcWaitNs) {
+    return mbar_try_wait(bar, parity) || tc_wait_long(bar, parity, gave_up, status, where, limit);
 }
-// The same for a block that has given up and still has copies or products in flight.
-static __device__ __noinline__ void tc_drain(uint64_t* bar, uint32_t parity) {
+// Whether all `threads` threads that share the named barrier say yes; each of them comes here, whatever its waits have said.
+__device__ __forceinline__ bool tc_agree(bool yes, int barrier, int threads) {
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(all) : "r"((uint32_t)yes), "r"(barrier), "r"(threads) : "memory");
+    return all != 0;
+}
+// For a block that has given up, between its last copy or product and the end of the memory these may still be at: they take microseconds.
+static __device__ __noinline__ void tc_settle() {
     const unsigned long long began = global_ns();
-    while (!mbar_try_wait(bar, parity) && global_ns() - began < kTcWaitNs) {}
+    while (global_ns() - began < kTcSettleNs) __nanosleep(1000);
 }
 
 // The same address in CTA `rank` of the cluster, and an arrival there.  (Its order reaches what this CTA has written to its own shared

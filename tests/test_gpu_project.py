@@ -774,6 +774,20 @@ def test_captured_calls_replay(ctx, tokens):
 
 
 @gpu
+def test_a_group_of_warps_whose_waits_end_differently(ctx):
+    """One warp of four waits in vain, the others do not wait: they leave together, the time-out is reported once, and the context goes on."""
+    p = Problem(ctx, 40, 128, 192, 8, BF16, 8, 2, [40], which=[1])
+    y, _ = check_forward(ctx, p)
+    launches = ctx.zipml_kernel_launches()
+    ctx.zipml_wait_probe(200_000)
+    with pytest.raises(binding.ZipmlError) as e:
+        ctx.zipml_sync()
+    assert e.value.code == binding.ERR_TIMEOUT and ctx.zipml_kernel_launches() == launches + 2
+    again, _ = check_forward(ctx, p)
+    assert torch.equal(again, y)
+
+
+@gpu
 def test_two_contexts_at_once():
     """Two streams, a context each, their calls interleaved: each has its own workspace."""
     streams = [torch.cuda.Stream() for _ in range(2)]
