@@ -145,14 +145,15 @@ def _ptr(t, dtype=None, device=None):
 
 
 def _rows(t, device):
-    """(address, dtype, rows, columns, leading dimension) of a matrix whose rows are contiguous."""
+    """(address, dtype, rows, columns, leading dimension) of a matrix whose rows are contiguous and do not overlap (an expanded one's do)."""
     rows, columns = t.shape
     ld, unit = t.stride()
     dtype = DTYPES.get(t.dtype)
     assert dtype is not None, f"expected one of {sorted(map(str, DTYPES))}, got {t.dtype}"
     assert t.device == device, f"expected a tensor on {device}, got {t.device}"
     assert unit == 1 or columns <= 1, "rows must be contiguous"
-    return t.data_ptr(), dtype, rows, columns, ld if rows > 1 and ld > columns else columns
+    assert ld >= columns or rows <= 1, "rows must not overlap"
+    return t.data_ptr(), dtype, rows, columns, ld if rows > 1 else columns
 
 
 class Checkpoint:

@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_1611_05402_b200 import binding
 
@@ -109,3 +110,28 @@ def test_projection_arguments(lib, ctx):
     for kw in (dict(dy=None), dict(dy=AT + 1), dict(dx=AT), dict(dx=AT + 1), dict(lddy=47), dict(lddx=63), dict(hidden=None), dict(cp=None), dict(ga=AT + 2),
                dict(gb=AT + 2), dict(cp=checkpoint(n=63)), dict(cp=checkpoint(m=9)), dict(none=True)):
         assert backward(lib, ctx, **kw) == BAD, kw
+
+
+CPU = torch.device("cpu")
+
+
+@pytest.mark.parametrize("matrix", [
+    torch.zeros(8).expand(5, 8),                             # what autograd gives a sum over rows: every row the same memory
+    torch.zeros(1, 1).expand(5, 1),
+    torch.zeros(40).as_strided((5, 8), (7, 1)),              # each row begins in the one before
+    torch.zeros(40).as_strided((5, 8), (1, 1)),
+    torch.zeros(8, 5).t(),                                   # columns contiguous, not rows
+    torch.zeros(5, 16)[:, ::2],
+    torch.zeros(5, 8, dtype=torch.float64),
+], ids=["expanded", "expanded column", "overlapping", "sliding", "transposed", "every other column", "fp64"])
+def test_matrices_that_are_not_rows(matrix):
+    with pytest.raises(AssertionError):
+        binding._rows(matrix, CPU)
+
+
+@pytest.mark.parametrize("matrix,ld", [
+    (torch.zeros(5, 8), 8), (torch.zeros(5, 16)[:, 3:11], 16), (torch.zeros(1, 8), 8), (torch.zeros(8).expand(1, 8), 8), (torch.zeros(40).as_strided((1, 8), (3, 1)), 8),
+    (torch.zeros(10, 8)[::2], 16), (torch.zeros(5, 1), 1), (torch.zeros(5, 4)[:, :1], 4), (torch.zeros(0, 8), 8)],
+    ids=["whole", "columns of a wider one", "a row", "an expanded row", "a row of any stride", "every other row", "a column", "a column of a wider one", "no rows"])
+def test_matrices_that_are_rows(matrix, ld):
+    assert binding._rows(matrix, CPU) == (matrix.data_ptr(), binding.F32, *matrix.shape, ld)
