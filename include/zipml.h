@@ -393,8 +393,8 @@ typedef struct zipml_adapters {
     int32_t requests;       /* >= 1                                                                  */
     int32_t reserved;       /* 0                                                                     */
     const int32_t* starts;  /* requests + 1                                                          */
-    const int32_t* which;   /* requests; an index >= count counts as none and makes the next zipml_sync() return
-                               ZIPML_ERR_INVALID_ARG                                                 */
+    const int32_t* which;   /* requests; an index >= count counts as none and, where the request holds tokens, makes the
+                               next zipml_sync() return ZIPML_ERR_INVALID_ARG                        */
 } zipml_adapters;
 
 /* zipml_project: Y[t] = W^T x_t + b_i^T h_t with h_t = scale_i a_i x_t for the adapter i of token t.

@@ -112,9 +112,14 @@ __device__ __forceinline__ void grad_pass(const GradArgs& a, const CUtensorMap* 
         {
             const int req = first + (int)threadIdx.x;
             int s = 0, e = 0;
-            if (req < a.requests && a.which[req] == adapter) {
+            const int which = req < a.requests ? a.which[req] : -1;
+            if (which == adapter || which >= a.adapters) {
                 s = max(a.starts[req], 0);
                 e = (int)min((int64_t)a.starts[req + 1], a.tokens);
+            }
+            if (which >= a.adapters) {                     // (the first stage reports it too, but a call that wants grad_up alone has none)
+                if (e > s) set_status(a.status, ZIPML_ERR_INVALID_ARG, 91);
+                e = s;
             }
             const uint32_t has = __ballot_sync(0xffffffffu, e > s);
             if (lane == 0) sh.found[warp] = __popc(has);

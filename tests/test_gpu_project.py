@@ -432,6 +432,27 @@ def test_an_index_past_the_adapters_counts_as_none(ctx):
 
 
 @gpu
+@pytest.mark.parametrize("wanted", ["dx", "grad_a", "grad_b", "all"])
+@pytest.mark.parametrize("tokens", [30, 300])
+def test_an_index_past_the_adapters_is_reported_by_every_part_of_the_backward_pass(ctx, tokens, wanted):
+    p = Problem(ctx, tokens, 96, 64, 8, BF16, 4, 2, [10, tokens - 10, 0], which=[1, 2, 5])
+    hidden, cp = torch.ones(tokens, 4, device=ctx.device), ctx.zipml_checkpoint_encode(p.x, group=32)
+    kw = dict(adapters=p.adapters, starts=p.starts, which=p.which, want_input=wanted in ("dx", "all"))
+    if wanted in ("grad_a", "all"):
+        kw["checkpoint"] = cp
+    if wanted in ("grad_b", "all"):
+        kw["hidden"] = hidden
+    first = ctx.zipml_project_backward(p.weights, p.dy, **kw)
+    with pytest.raises(binding.ZipmlError) as e:
+        ctx.zipml_sync()
+    assert e.value.code == binding.ERR_INVALID_ARG
+    p.which[1] = -1                                                             # (the empty request's index is nobody's)
+    again = ctx.zipml_project_backward(p.weights, p.dy, **kw)
+    ctx.zipml_sync()
+    assert all(u is None if v is None else torch.equal(u, v) for u, v in zip(first, again))
+
+
+@gpu
 @pytest.mark.parametrize("tokens", [12, 200])
 def test_what_is_not_finite_stays_with_its_request(ctx, tokens):
     p = Problem(ctx, tokens, 192, 256, 8, F16, 8, 2, [tokens // 2, tokens - tokens // 2], which=[0, 1])
