@@ -413,6 +413,7 @@ typedef struct zipml_adapters {
  *   The gradients are written whole, zero for adapters without tokens.
  * Products of 16-bit values and of codes are exact and summed in fp32; h_t and v_t are kept in fp32 and enter the second product as two
  * 16-bit parts, and so does dY times the outputs' steps (off by at most 2^-21 of a row's largest).  Results do not change from call to call.
+ * Sums run in fp32: a row whose magnitudes add up to more than that holds may come out infinite.
  * An infinity or a NaN in a token's row stays in that row (and in the gradients of its adapter); one in an adapter's factor b (backward: a)
  * counts as zero in the product behind it and makes the next zipml_sync() return ZIPML_ERR_NONFINITE.
  * tokens = 0 is allowed (gradients are then zero).  Workspace grows on a call that needs more than any before it; while the stream is being

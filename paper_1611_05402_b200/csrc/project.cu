@@ -50,6 +50,7 @@ constexpr int kProjThreads = 32 * (kSecondIssuer + 1);
 constexpr int kMostSlots = 12;
 constexpr int kRankChunk = 32;                // ranks of an adapter stage: high parts in the first half of the depth, low ones in the second
 constexpr uint32_t kLeftBytes = kProjRows * kProjDepth * 2;
+constexpr float kCodeScale = 256.0f;          // of codes beside bf16 tokens (see centred_pair)
 
 // Slots of the rings.  The left operand's is the deepest: unpacking a stage takes some 1,000 cycles from its codes' arrival to its last
 // store, two products' worth, where a tensor copy of tokens only has L2's latency to cover.  A stage has one barrier that tells that both of
@@ -142,10 +143,11 @@ __device__ __forceinline__ void codes_to_bytes(uint32_t (&w)[4]) {
     }
 }
 
-// Two codes, in the low bytes of p's halves under the byte of 128 (bf16) or 1024 (fp16), as code - center: the code is the mantissa's
-// lowest bits, and one exact subtraction of `base` = that and the center takes the offset away.  EIGHT: 8-bit codes in bf16, whose mantissa has 7
-// bits: a code's top bit counts as exponent there, and the value is 128 + code below 128, 256 + 2 (code - 128) from there on; less 256
-// it is what it should be, or twice that.  (Byte and logic instructions run at half the rate of the 16-bit arithmetic's and bound the
+// Two codes, in the low bytes of p's halves under the byte of 1/2 (bf16) or 1024 (fp16), as code - center, bf16's times 2^-8: the code is the mantissa's
+// lowest bits, and one exact subtraction of `base` = that and the center takes the offset away.  (2^-8: a product with a bf16 token is then no
+// larger than the token, which may be anything that fp32 holds; kCodeScale in the epilogue takes it back.)  EIGHT: 8-bit codes in bf16, whose mantissa
+// has 7 bits: a code's top bit counts as exponent there, and the value is 128 + code below 128, 256 + 2 (code - 128) from there on, times 2^-8;
+// less 256 it is what it should be, or twice that.  (Byte and logic instructions run at half the rate of the 16-bit arithmetic's and bound the
 // unpacking: two of each a pair.)
 template <bool BF16, bool EIGHT>
 __device__ __forceinline__ uint32_t centred_pair(uint32_t p, uint32_t base) {
@@ -163,14 +165,14 @@ __device__ __forceinline__ uint32_t centred_pair(uint32_t p, uint32_t base) {
 }
 template <bool BF16, bool EIGHT>
 __device__ __forceinline__ uint4 centred_chunk(uint32_t w0, uint32_t w1, uint32_t base) {      // 8 codes
-    constexpr uint32_t kTop = BF16 ? 0x43434343u : 0x64646464u;
+    constexpr uint32_t kTop = BF16 ? 0x3F3F3F3Fu : 0x64646464u;
     return make_uint4(centred_pair<BF16, EIGHT>(__byte_perm(w0, kTop, 0x4140), base), centred_pair<BF16, EIGHT>(__byte_perm(w0, kTop, 0x4342), base),
                       centred_pair<BF16, EIGHT>(__byte_perm(w1, kTop, 0x4140), base), centred_pair<BF16, EIGHT>(__byte_perm(w1, kTop, 0x4342), base));
 }
-// The base for codes of so many bits, in both halves: 128 (256 for EIGHT) or 1024, and the center 2^(bits - 1).
+// The base for codes of so many bits, in both halves: 128 (256 for EIGHT), times 2^-8, or 1024, and the center 2^(bits - 1).
 template <bool BF16>
 __device__ __forceinline__ uint32_t centre_base(int bits) {
-    const uint32_t center = 1u << (bits - 1), h = BF16 ? 0x4300u + center : 0x6400u + center;      // (8 bits in bf16: 0x4380, which is 256)
+    const uint32_t center = 1u << (bits - 1), h = BF16 ? 0x3F00u + center : 0x6400u + center;      // (8 bits in bf16: 0x3F80, which is 256 times 2^-8)
     return h | h << 16;
 }
 
@@ -471,6 +473,7 @@ __global__ void __launch_bounds__(kProjThreads, 1) project_kernel(ProjectArgs a,
         if (a.step && feature < a.features) {
             alpha = a.step[feature];
             beta = fmaf(a.center, alpha, a.lo[feature]);
+            if constexpr (BF16) alpha *= kCodeScale;
         }
         // (a warp gives up as a whole; the next stage's codes are on their way into registers while this one's are unpacked)
         const auto unpack = [&](auto container, auto eight) {

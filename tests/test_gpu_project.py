@@ -505,6 +505,34 @@ def test_magnitudes_at_the_ends_of_fp16(ctx, factor):
 
 
 @gpu
+@pytest.mark.parametrize("tokens,inputs,outputs,bits", [(1, 200, 72, 8), (40, 512, 256, 4), (100, 200, 264, 8), (300, 136, 264, 6), (1400, 2304, 2304, 8)])
+@pytest.mark.parametrize("size", [3e38, 1e-35])
+def test_magnitudes_at_the_ends_of_bf16(ctx, tokens, inputs, outputs, bits, size):
+    """A token may be as large as its type allows, as long as its own sum and the result are within fp32; and small ones lose nothing."""
+    p = Problem(ctx, tokens, inputs, outputs, bits, BF16, 8, 2, [tokens], which=[1], group=64)
+    g = torch.Generator().manual_seed(8)
+    at, row = torch.randint(0, inputs, (tokens,), generator=g).to(ctx.device), torch.arange(tokens, device=ctx.device)
+    p.b /= 8                                                                    # (the adapters' term would leave bf16)
+    x = p.x.double()
+    if size > 1:
+        p.x[:] = (x / x.abs().max() * (size / 64 / inputs)).to(BF16)
+        p.x[row, at] = size
+        p.dy[:] = (p.dy.double() / p.dy.double().abs().max() * (size / 64 / outputs)).to(BF16)
+        p.dy[row, at % outputs] = -size
+    else:
+        p.x[:] = (x * size).to(BF16)
+        p.dy[:] = (p.dy.double() * size).to(BF16)
+    hidden = torch.zeros(tokens, 8, device=ctx.device)
+    kw = dict(adapters=p.adapters, starts=p.starts, which=p.which)
+    y = ctx.zipml_project(p.weights, p.x, hidden=hidden, **kw)
+    dx = ctx.zipml_project_backward(p.weights, p.dy, **kw)[0]
+    ctx.zipml_sync()
+    for got, want in ((y, p.forward()[0]), (dx, p.backward(hidden, ctx.zipml_checkpoint_encode(torch.zeros_like(p.x), group=64))[0])):
+        assert want.abs().max() < 3e38 and torch.isfinite(got).all()
+        assert ((got.double() - want) / size).norm() <= (half_step(BF16) + 2.0**-17) * (want / size).norm()
+
+
+@gpu
 def test_no_tokens(ctx):
     p = Problem(ctx, 4, 64, 80, 8, BF16, 8, 2, [4])
     empty = p.x[:0]
