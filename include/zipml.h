@@ -417,8 +417,8 @@ typedef struct zipml_adapters {
  * An infinity or a NaN in a token's row stays in that row (and in the gradients of its adapter); one in an adapter's factor b (backward: a)
  * counts as zero in the product behind it and makes the next zipml_sync() return ZIPML_ERR_NONFINITE.
  * tokens = 0 is allowed (gradients are then zero).  Workspace grows on a call that needs more than any before it; while the stream is being
- * captured that is refused with ZIPML_ERR_WORKSPACE (make one call of that size first).  Earlier blocks live as long as the context, so
- * recorded launches keep theirs; graphs recorded from one context share them and must not run at the same time.
+ * captured that is refused with ZIPML_ERR_WORKSPACE (make one call of that size first).  Blocks that recorded launches use live as long as the context;
+ * graphs recorded from one context share them with each other and with the context's calls: none of these may run at the same time.
  * ZIPML_ERR_UNSUPPORTED: level tables, other layouts or types; ZIPML_ERR_WORKSPACE: inputs or outputs above 2^24, tokens above
  * 2^30. */
 int zipml_project(zipml_ctx* ctx, const zipml_dataset* weights, const zipml_adapters* adapters, const void* X, int32_t dtype, int64_t tokens,

@@ -49,17 +49,35 @@ int allow_shared(zipml_ctx* ctx, const void* kernel, size_t bytes) {
 }
 
 int project_reserve(zipml_ctx* ctx, size_t bytes, unsigned char** block) {
+    const bool recording = capturing(ctx);
     if (bytes > ctx->project_bytes || ctx->project_blocks == 0) {
-        if (capturing(ctx) || ctx->project_blocks == zipml_ctx::kProjectBlocks) return ZIPML_ERR_WORKSPACE;
-        size_t want = bytes > 2 * ctx->project_bytes ? bytes : 2 * ctx->project_bytes;
-        want = (want + (1u << 20) - 1) >> 20 << 20;
-        if (want == 0) want = 1u << 20;
+        if (recording) return ZIPML_ERR_WORKSPACE;
+        const size_t had = ctx->project_bytes;
+        if (ctx->project_blocks > 0 && !ctx->project_recorded) {
+            cudaError_t e = cudaStreamSynchronize(ctx->stream);           // (earlier work may still use it)
+            if (e != cudaSuccess) return cuda_status(e);
+            ctx->project_bytes = 0;
+            ctx->project_recorded = true;                                 // (as the blocks before it are)
+            e = cudaFree(ctx->project_ws[--ctx->project_blocks]);
+            if (e != cudaSuccess) return cuda_status(e);
+        }
+        if (ctx->project_blocks == zipml_ctx::kProjectBlocks) return ZIPML_ERR_WORKSPACE;
+        // twice the last one, so that calls that grow bit by bit allocate seldom; what is needed where that much is not to be had
+        const auto megabytes = [](size_t n) { return n == 0 ? (size_t)1 << 20 : (n + (1u << 20) - 1) >> 20 << 20; };
+        size_t want = megabytes(bytes > 2 * had ? bytes : 2 * had);
         unsigned char* fresh = nullptr;
-        const cudaError_t e = cudaMalloc(reinterpret_cast<void**>(&fresh), want);
+        cudaError_t e = cudaMalloc(reinterpret_cast<void**>(&fresh), want);
+        if (e == cudaErrorMemoryAllocation && want > megabytes(bytes)) {
+            (void)cudaGetLastError();
+            want = megabytes(bytes);
+            e = cudaMalloc(reinterpret_cast<void**>(&fresh), want);
+        }
         if (e != cudaSuccess) return cuda_status(e);
         ctx->project_ws[ctx->project_blocks++] = fresh;
         ctx->project_bytes = want;
+        ctx->project_recorded = false;
     }
+    ctx->project_recorded |= recording;
     *block = ctx->project_ws[ctx->project_blocks - 1];
     return ZIPML_OK;
 }

@@ -34,12 +34,13 @@ struct zipml_ctx {
     const char* last_kernel = "";
     void ran(int engine, const char* kernel) { last_engine = engine; last_kernel = kernel; }
     void* tmap_encode = nullptr;    // cuTensorMapEncodeTiled, resolved on first use
-    // workspace of the projections: its blocks live as long as the context (recorded launches hold their addresses), the last one is
-    // the largest, each at least twice the one before
+    // workspace of the projections: the last block is the one in use and the largest; those before it are held by recorded launches, which know
+    // their addresses, and live as long as the context
     static constexpr int kProjectBlocks = 44;
     unsigned char* project_ws[kProjectBlocks] = {};
     int project_blocks = 0;
-    size_t project_bytes = 0;
+    size_t project_bytes = 0;       // of the last one
+    bool project_recorded = false;  // the last one is held too
     const void* allowed[64] = {};   // kernels that have been allowed their shared memory (see allow_shared), by hash, the newest wins
 };
 

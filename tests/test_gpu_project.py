@@ -883,6 +883,64 @@ def test_capture_refuses_to_grow_the_workspace():
         del graph
 
 
+def backward_of(c, tokens):
+    """A call that needs 4 bytes of workspace for each of tokens x 16,384 and little else, its result, and what its last rows should be."""
+    w = c.zipml_quantize(torch.randn(64, 16384, generator=torch.Generator().manual_seed(1)).to("cuda:0"), 4, seed=1)
+    dy = torch.empty(tokens, 16384, dtype=BF16, device="cuda:0").normal_(generator=torch.Generator("cuda:0").manual_seed(2))
+    out = torch.zeros(tokens, 64, dtype=BF16, device="cuda:0")
+
+    def check():
+        c.zipml_sync()
+        beta, step, codes = weight_parts(w)
+        want = dy[-100:].double() @ (beta + step * codes).T
+        assert (out[-100:].double() - want).norm() <= (half_step(BF16) + 2.0**-17) * want.norm()
+    return lambda: c.zipml_project_backward(w, dy, out=out), out, check
+
+
+def free_bytes():
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    return torch.cuda.mem_get_info()[0]
+
+
+@gpu
+def test_the_workspace_grows_without_keeping_what_nobody_uses():
+    with binding.Context("cuda:0") as c:
+        calls = [backward_of(c, tokens) for tokens in (300, 16384, 17000, 33000)]
+        calls[0][0]()
+        before = free_bytes()
+        for call, _, check in calls:
+            call()
+            check()
+        # somewhat more than 1 GiB and 2 GiB are needed: one block, of no more than twice the 2 GiB
+        assert before - free_bytes() <= (4 << 30) + (128 << 20)
+
+
+@gpu
+@pytest.mark.parametrize("recorded", [False, True])
+def test_the_workspace_grows_to_what_is_needed_where_twice_the_last_is_not_there(recorded):
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream), binding.Context("cuda:0", stream=stream) as c:
+        (first, y, check), (second, _, check_second) = backward_of(c, 32768), backward_of(c, 34000)
+        first()
+        check()
+        graph = torch.cuda.CUDAGraph() if recorded else None
+        if recorded:
+            with torch.cuda.graph(graph, stream=stream):
+                first()
+        # 2 GiB are in use and a little more is needed: beside them where a graph holds them, else in their place
+        ballast = torch.empty(free_bytes() - ((3 << 30) if recorded else (3 << 29)), dtype=torch.uint8, device="cuda:0")
+        second()
+        check_second()
+        del ballast
+        torch.cuda.empty_cache()
+        if recorded:
+            y.zero_()
+            graph.replay()
+            check()
+            del graph
+
+
 @gpu
 def test_refusals(ctx):
     p = Problem(ctx, 10, 64, 64, 8, BF16, 8, 2, [10])
