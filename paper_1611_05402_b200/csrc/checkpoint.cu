@@ -172,7 +172,9 @@ __global__ void __launch_bounds__(32 * kEncodeWarps) checkpoint_encode_kernel(co
         }
         if (j < a.row_bytes) *reinterpret_cast<uint4*>(a.codes + row * a.row_bytes + j) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
         if (count > 0 && (lane & (lanes - 1)) == 0) {
-            a.grids[row * a.groups + j / a.group] = make_float2(lo, step);
+            // (the roundings of range and step may take the upper end past the largest number: a step's last place keeps it there)
+            const bool past = !(__fmaf_rn(255.0f, step, lo) <= kMostFloat);
+            a.grids[row * a.groups + j / a.group] = make_float2(lo, past ? __uint_as_float(__float_as_uint(step) - 1u) : step);
             bad |= !(range <= kMostFloat);
         }
     }

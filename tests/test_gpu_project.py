@@ -266,6 +266,21 @@ def test_checkpoint_of_constant_tiny_and_large_groups(ctx):
 
 
 @gpu
+def test_checkpoint_of_the_largest_numbers(ctx):
+    """Whatever fp32 holds comes back within fp32, where roundings of the grid would lead past its end too (about one in 25 of these groups)."""
+    top = np.finfo(np.float32).max
+    low = np.concatenate([[2.2058903e+35, 0.0, -1e31], 10.0 ** np.random.RandomState(1).uniform(25, 38.4, 400)]).astype(np.float32)
+    x = torch.from_numpy(np.stack([np.linspace(float(v), float(top), 32).astype(np.float32) for v in low]))
+    x[:, -1] = float(top)
+    cp = ctx.zipml_checkpoint_encode(x.to(ctx.device), group=32, seed=6)
+    back = ctx.zipml_checkpoint_decode(cp, dtype=F32)
+    ctx.zipml_sync()
+    assert torch.isfinite(back).all()
+    lo, step, c = checkpoint_values(cp)
+    assert ((back.double() - x.double().to(ctx.device)).abs() <= step * (1 + 1e-5) + 2.0**-22 * float(top)).all()
+
+
+@gpu
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 def test_checkpoint_reports_what_is_not_finite(ctx, bad):
     x = torch.randn(40, 300, device=ctx.device)
