@@ -759,6 +759,199 @@ def test_results_where_the_codes_and_the_lower_ends_cancel(ctx, tokens, inputs, 
         assert beyond_rounding(got, want) <= rounded_elsewhere(dtype, 2.0**-16 + parts.item() * lost)
 
 
+@gpu
+@pytest.mark.parametrize("tokens,inputs,outputs,rank,group", [(40, 8192, 72, 16, 128), (257, 16500, 72, 5, 256), (520, 8192, 264, 33, 128), (300, 72, 8192, 16, 64), (6000, 264, 200, 16, 128),
+                                                              (6000, 264, 200, 40, 32)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_results_in_fp32_hold_what_fp32_holds(ctx, tokens, inputs, outputs, rank, group, dtype):
+    """hidden and the adapters' gradients against 64 bits, in relation to the whole.  A sum of k roundings in a row is off by sqrt(k) 2^-24 or so; 2e-6, 34 of
+    them, is below what any of the long sums here would lose to the tensor cores' cutting, or the products to a missing low part (2^-12)."""
+    p = Problem(ctx, tokens, inputs, outputs, 8, dtype, rank, 2, [tokens // 3, tokens - tokens // 3], which=[1, 0], group=group)
+    kw = dict(adapters=p.adapters, starts=p.starts, which=p.which)
+    hidden = torch.zeros(tokens, rank, device=ctx.device)
+    ctx.zipml_project(p.weights, p.x, hidden=hidden, **kw)
+    cp = ctx.zipml_checkpoint_encode(p.x, group=group, seed=5)
+    _, da, db = ctx.zipml_project_backward(p.weights, p.dy, hidden=hidden, checkpoint=cp, **kw)
+    ctx.zipml_sync()
+    ref = p.backward(hidden, cp)
+    for got, want in ((hidden, p.forward()[2]), (da, ref[2]), (db, ref[4])):
+        assert (got.double() - want).norm() <= 2e-6 * want.norm()
+
+
+# --- many tokens: what tiles of 128 and pairs of tiles do with rows and values that are not theirs -------------------------------------
+
+def spread_out(ctx, tokens, inputs, outputs, dtype, rank=16):
+    """Three requests with tokens, one of them without an adapter, and an empty one; rows before the first and behind the last."""
+    return Problem(ctx, tokens, inputs, outputs, 8, dtype, rank, 3, [tokens // 3, 0, tokens // 4, tokens - tokens // 3 - tokens // 4 - 117], which=[1, 2, -1, 0], first=37, group=64)
+
+
+MANY = [(300, 264, 520), (601, 264, 520), (1500, 2304, 2304)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("tokens,inputs,outputs", MANY)
+def test_many_tokens_and_rows_outside_the_requests(ctx, tokens, inputs, outputs, dtype):
+    p = spread_out(ctx, tokens, inputs, outputs, dtype)
+    assert int(p.outside.sum()) == 117
+    p.x[p.outside] = float("nan")
+    p.dy[p.outside] = float("-inf")
+    check_forward(ctx, p)
+    p.x[p.outside] = 0.0                                                        # (the checkpoint reports what is not finite)
+    _, da, _ = check_backward(ctx, p)
+    assert (da[2] == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("tokens,inputs,outputs", MANY)
+def test_many_tokens_and_what_is_not_finite(ctx, tokens, inputs, outputs, dtype):
+    p = spread_out(ctx, tokens, inputs, outputs, dtype)
+    kw = dict(adapters=p.adapters, starts=p.starts, which=p.which)
+    hidden, cp = torch.ones(tokens, 16, device=ctx.device), ctx.zipml_checkpoint_encode(p.x, group=64)
+
+    def calls():
+        out = torch.full((tokens, outputs), 3.0, dtype=dtype, device=ctx.device), torch.full((tokens, inputs), 3.0, dtype=dtype, device=ctx.device)
+        ctx.zipml_project(p.weights, p.x, out=out[0], **kw)
+        dx, da, db = ctx.zipml_project_backward(p.weights, p.dy, hidden=hidden, checkpoint=cp, out=out[1], **kw)
+        ctx.zipml_sync()
+        return (*out, da, db)
+
+    first = calls()
+    assert all(torch.isfinite(t).all() for t in first)
+    # in two rows, of the first request and the last
+    at = [int(p.starts[0]) + 3, int(p.starts[-1]) - 2]
+    kept = p.x[at].clone(), p.dy[at].clone()
+    p.x[at[0], 3] = float("inf")
+    p.x[at[1], 4] = float("nan")
+    p.dy[at[0], 5] = float("nan")
+    p.dy[at[1], 6] = float("-inf")
+    got = calls()
+    rest = [t for t in range(tokens) if t not in at]
+    for u, v in zip(got[:2], first[:2]):
+        assert torch.equal(u[rest], v[rest]) and not torch.isfinite(u[at]).any()
+    for u, v in zip(got[2:], first[2:]):                                        # (adapters 1 and 0 have taken them in)
+        assert torch.equal(u[2], v[2]) and not torch.isfinite(u[0]).all() and not torch.isfinite(u[1]).all()
+    p.x[at], p.dy[at] = kept
+    # in an adapter's factors: the other requests' rows and gradients stay as they were
+    others = torch.tensor(p.ids != 1, device=ctx.device)
+    for name in ("a", "b"):
+        factor = getattr(p, name)
+        kept = factor.clone()
+        factor[1, 2, 7] = float("nan")
+        factor[1, 3, 9] = float("inf")
+        y = torch.full((tokens, outputs), 3.0, dtype=dtype, device=ctx.device)
+        dx = torch.full((tokens, inputs), 3.0, dtype=dtype, device=ctx.device)
+        ctx.zipml_project(p.weights, p.x, out=y, **kw)
+        forward = binding.OK
+        try:
+            ctx.zipml_sync()
+        except binding.ZipmlError as e:
+            forward = e.code
+        _, da, db = ctx.zipml_project_backward(p.weights, p.dy, hidden=hidden, checkpoint=cp, out=dx, **kw)
+        backward = binding.OK
+        try:
+            ctx.zipml_sync()
+        except binding.ZipmlError as e:
+            backward = e.code
+        # the second product's factor counts as zero where it is not finite, and is reported; the first one's reaches its own tokens
+        assert (forward, backward) == ((binding.OK, binding.ERR_NONFINITE) if name == "a" else (binding.ERR_NONFINITE, binding.OK))
+        assert torch.equal(y[others], first[0][others]) and torch.equal(dx[others], first[1][others])
+        assert torch.equal(da[0], first[2][0]) and torch.equal(db, first[3])
+        factor.copy_(kept)
+    assert all(torch.equal(u, v) for u, v in zip(calls(), first))
+
+
+@gpu
+@pytest.mark.parametrize("tokens,inputs,outputs", MANY)
+def test_many_tokens_and_parts_of_the_backward_pass(ctx, tokens, inputs, outputs):
+    p = spread_out(ctx, tokens, inputs, outputs, BF16)
+    hidden = torch.ones(tokens, 16, device=ctx.device)
+    dx, da, db = check_backward(ctx, p, hidden=hidden)
+    cp = ctx.zipml_checkpoint_encode(p.x, group=p.group, seed=5)
+    kw = dict(adapters=p.adapters, starts=p.starts, which=p.which)
+    only = ctx.zipml_project_backward(p.weights, p.dy, checkpoint=cp, want_input=False, **kw)
+    assert only[0] is None and only[2] is None and torch.equal(only[1], da)
+    only = ctx.zipml_project_backward(p.weights, p.dy, hidden=hidden, want_input=False, **kw)
+    assert only[0] is None and only[1] is None and torch.equal(only[2], db)
+    only = ctx.zipml_project_backward(p.weights, p.dy, out=torch.full_like(dx, 3.0), **kw)
+    assert torch.equal(only[0], dx) and only[1] is None and only[2] is None
+    ctx.zipml_sync()
+
+
+@gpu
+@pytest.mark.parametrize("rank,count,requests", [(1, 1, 1), (1, 3, 2), (3, 1, 4), (128, 1, 1), (12, 9, 9)])
+def test_many_tokens_and_adapters_of_any_shape(ctx, rank, count, requests):
+    lengths = [600 // requests] * requests
+    p = Problem(ctx, 600, 264, 520, 4, BF16, rank, count, lengths, which=[i % count for i in range(requests)], group=128)
+    check_forward(ctx, p)
+    check_backward(ctx, p)
+
+
+@gpu
+@pytest.mark.parametrize("tokens,requests,count", [(700, 5000, 3), (1000, 1000, 1000), (5, 700, 2000)])
+def test_many_requests_and_adapters(ctx, tokens, requests, count):
+    """More requests than a pass of any kernel looks at together, most of them empty, and adapters that nobody uses."""
+    lengths = np.random.RandomState(requests).multinomial(tokens, np.ones(requests) / requests).tolist()
+    p = Problem(ctx, tokens, 72, 136, 8, F16, 4, count, lengths, group=32)
+    check_forward(ctx, p)
+    check_backward(ctx, p)
+
+
+@gpu
+@pytest.mark.parametrize("tokens", [5, 600])
+def test_outputs_whose_weights_are_all_the_same(ctx, tokens):
+    """A step of zero: the codes say nothing and the lower end is the weight."""
+    p = Problem(ctx, tokens, 200, 136, 8, BF16, 8, 2, [tokens])
+    p.weights.feat_step[5:40] = 0.0
+    check_forward(ctx, p)
+    check_backward(ctx, p)
+    p.weights.feat_step.zero_()
+    check_forward(ctx, p)
+    check_backward(ctx, p)
+
+
+@gpu
+@pytest.mark.parametrize("tokens,inputs,outputs", MANY)
+def test_captured_calls_of_many_tokens_replay(ctx, tokens, inputs, outputs):
+    """Calls recorded at one division of the tokens run at another: what the device holds when they run counts."""
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream), binding.Context("cuda:0", stream=stream) as c:
+        p = spread_out(c, tokens, inputs, outputs, BF16)
+        results = [torch.zeros(*shape, dtype=dtype, device="cuda:0") for shape, dtype in (((tokens, outputs), BF16), ((tokens, 16), F32), ((tokens, inputs), BF16),
+                                                                                       (p.a.shape, F32), (p.b.shape, F32))]
+        y, hidden, dx, da, db = results
+        cp = c.zipml_checkpoint_encode(p.x, group=64, seed=4)
+
+        def calls():
+            c.zipml_checkpoint_encode(p.x, group=64, seed=4, out=cp)
+            c.zipml_project(p.weights, p.x, adapters=p.adapters, starts=p.starts, which=p.which, out=y, hidden=hidden)
+            c.zipml_project_backward(p.weights, p.dy, adapters=p.adapters, starts=p.starts, which=p.which, hidden=hidden, checkpoint=cp, out=dx, grad_a=da, grad_b=db)
+
+        calls()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            calls()
+        for starts in ([37, 100, 150, 200, tokens], [0, 0, tokens // 2, tokens // 2, tokens - 1]):
+            p.starts.copy_(torch.tensor(starts, dtype=torch.int32))
+            p.x.copy_(torch.randn_like(p.x))
+            p.dy.copy_(torch.randn_like(p.dy))
+            got = []
+            for run in (graph.replay, calls):
+                for t in results:
+                    t.fill_(3.0)
+                run()
+                stream.synchronize()
+                c.zipml_sync()
+                got.append([t.clone() for t in results])
+            assert all(torch.equal(u, v) for u, v in zip(*got))
+            held = torch.zeros(tokens, dtype=torch.bool, device="cuda:0")
+            held[starts[0]:starts[-1]] = True
+            assert all((t[~held] == 3.0).all() for t in results[:3])
+        del graph
+
+
 # --- how calls are made -----------------------------------------------------------------------------------------------------------
 
 @gpu
