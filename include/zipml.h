@@ -369,11 +369,12 @@ typedef struct zipml_checkpoint {
 /* zipml_checkpoint_encode: rounds X (m x n of type dtype, leading dimension ldx >= n) stochastically onto 8 bits, once, into the
  *   caller's buffers behind the const pointers of `out` (codes fully written, padding zero).  A group's grid has 255 intervals
  *   on its own range; a value goes to the lower or upper neighbouring level with the probabilities that make the
- *   expectation equal to the value up to 2^-16 of an interval (paper Section 2.1), so a gradient that is linear in the
- *   activations stays unbiased (the argument of Section 2.2).  Bits of Philox4x32-10 keyed by (seed, row, feature): the same
- *   seed gives the same codes; take another for each matrix and step.  A NaN, an infinity or a group whose range overflows
- *   fp32 makes the next zipml_sync() return ZIPML_ERR_NONFINITE (outputs undefined).
- * zipml_checkpoint_decode: the values lo + code * step as `dtype`, rounded once.
+ *   expectation equal to the value up to 2^-16 of an interval (paper Section 2.1; a group whose range is below 7.5e-37 keeps
+ *   fewer levels, and its values come back up to that range too low), so a gradient that is linear in the activations stays
+ *   unbiased (the argument of Section 2.2).  Bits of Philox4x32-10 keyed by (seed, row, feature): the same seed gives the same
+ *   codes; take another for each matrix and step, and not that of a zipml_quantize_draw with draw = 8.  A NaN, an infinity or a
+ *   group whose range overflows fp32 makes the next zipml_sync() return ZIPML_ERR_NONFINITE (outputs undefined).
+ * zipml_checkpoint_decode: the values lo + code * step, rounded to fp32 once and from there to `dtype`.
  * m = 0 is allowed and does nothing. */
 int zipml_checkpoint_encode(zipml_ctx* ctx, const void* X, int32_t dtype, int64_t m, int64_t n, int64_t ldx, uint64_t seed,
                             const zipml_checkpoint* out);

@@ -20,7 +20,7 @@ namespace zipml {
 constexpr int kEncodeWarps = 8;
 constexpr int kLaneFeatures = 16;
 constexpr int kWarpFeatures = 32 * kLaneFeatures;
-constexpr uint32_t kCheckpointDraws = 8;        // the Philox counter's last word (the quantizers use others)
+constexpr uint32_t kCheckpointDraws = 8;        // the Philox counter's last word (zipml_quantize_draw's draw 8 has the same)
 constexpr float kMostFloat = 3.402823466e38f;
 
 struct EncodeArgs {

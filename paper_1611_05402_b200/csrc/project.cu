@@ -36,8 +36,8 @@ namespace cg = cooperative_groups;
 // tile then waits for its start (2,000 cycles), the adapters (4,500) and the epilogue (7,500).  8192 x 8192 x 8192, 4 bits, rank 32: 776 us,
 // 1.43 PFLOP/s; 4096 tokens x 4096 x 16384, 8 bits, rank 16: 460 us; backward 8192 x 8192 x 8192, 8 bits: 1,359 us, whose
 // two parts' products run at 1.62 PFLOP/s (840 us with one part of 11 bits).  With single CTAs of 128 x 256, which read every token twice as often
-// from L2, the first took 990 us.  Few tokens: 470 to 530 cycles a stage against the 130 that the
-// codes' bytes would take; without the unpacking 285.
+// from L2, the first took 990 us.  Few tokens: some 500 cycles a stage against the 130 that the
+// codes' bytes would take; without the unpacking 285.  Backward, with two parts: 650 for 16 tokens, 750 for 64, 1,020 for 128, 1,060 for a pair.
 // ---------------------------------------------------------------------------------------------
 constexpr int kProjRows = 128;                // features of a CTA
 constexpr int kProjDepth = 64;                // depth of a stage: 128 bytes of 16-bit operand
@@ -876,9 +876,10 @@ static int launch_project_as(zipml_ctx* ctx, const ProjectArgs& a, const CUtenso
 
 // Tokens of a tile and CTAs that divide the depth, by the cycles that the waves of tiles should take, as measured: 480 a stage and 1 for every
 // token of a single CTA's tile, 580 for a pair's (backward, with two parts: 540 and 3, 1,060), and for a tile's start, adapters and
-// epilogue 4,500 and 42 for every token, where the depth is divided 1,500 more.  (Whole calls: 64 tokens x 4096 x 14336
-// 44 us with tiles of 64, 45 with 128, 98 with 16; 200 x 4096 x 4096 33 us with the depth divided, 38 without; 1000 x 4096 x 4096
-// 51 us by pairs, 68 with tiles of 128, 96 with 64.)
+// epilogue 4,500 and 42 for every token, where the depth is divided 1,500 more.  (Whole calls, one
+// after the other, rank 16: 64 tokens x 4096 x 14336 38 us with tiles of 64, 40 with 128, 92 with 16; 200 x 4096 x 4096 29 us with the depth
+// divided, 33 without; 1000 x 4096 x 4096 43 us by pairs, 64 with tiles of 128, 96 with 64.  Backward 64 x 4096 x 4096 37 us with the depth of tiles of
+// 64 divided by four, 45 with tiles of 16; 1000 x 4096 x 4096 84 us by pairs, 94 with 128; 2048 x 1000 x 1000 52 us with 128, 56 by pairs.)
 static void project_shape(const zipml_ctx* ctx, const ProjectArgs& a, bool backward, int* tokens, int* ranks, bool* pair) {
     const int64_t feature_tiles = (a.features + kProjRows - 1) / kProjRows, steps = (a.depth + kProjDepth - 1) / kProjDepth;
     double best = 0.0;

@@ -15,9 +15,6 @@ constexpr int kShrinkRows = 16;                 // tokens of a shrink tile: one 
 constexpr int kNoRequest = -2;                  // adapter index of a token that belongs to no request; -1: to one without an adapter
 
 // The dense floating types of activations and adapters.
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
-__device__ __forceinline__ float to_float(float v) { return v; }
 template <typename T> __device__ __forceinline__ T from_float(float v);
 template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }

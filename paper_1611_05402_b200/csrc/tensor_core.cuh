@@ -47,8 +47,9 @@ static __device__ __noinline__ void tc_settle() {
     while (global_ns() - began < kTcSettleNs) __nanosleep(1000);
 }
 
-// The same address in CTA `rank` of the cluster, and an arrival there.  (Its order reaches what this CTA has written to its own shared
-// memory, which is all that a pair's products read of it.  With .release.cluster an arrival took 2,000 cycles.)
+// The same address in CTA `rank` of the cluster, and an arrival there.  Its release has the default scope, a CTA's: that the products which the
+// other CTA issues then see what this one has stored to its own shared memory is an assumption about the hardware, which reads each CTA's half
+// where it lies, and not a guarantee of the memory model.  (With .release.cluster, which would be one, an arrival took 2,000 cycles.)
 __device__ __forceinline__ uint32_t tc_peer(const void* p, uint32_t rank) {
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
