@@ -272,7 +272,11 @@ class PreparedApply:
 
 
 class Context:
-    """zipml_create / zipml_destroy bound to torch's current stream of `device`."""
+    """zipml_create / zipml_destroy bound to torch's current stream of `device` (or to `stream`).
+
+    Calls enqueue there whatever torch's current stream is when they are made.  Made under another one, what they read has to be
+    ordered before them, and what torch allocates for their results belongs to that other stream: wait for an event, record_stream.
+    """
 
     def __init__(self, device="cuda:0", stream=None):
         self.device = torch.device(device)
